@@ -34,6 +34,11 @@ EMBEDDING = 2
 RMSNORM = 3
 LAYERNORM = 4
 
+ACT_NONE = 0
+ACT_RELU = 1
+ACT_GELU = 2
+ACT_SILU = 3
+
 PLAN_GREEDY = 0
 PLAN_TRAINING_COST = 1
 PLAN_BALANCED = 2
@@ -80,6 +85,23 @@ class GroupSegment(C.Structure):
 class ScheduleEntry(C.Structure):
     _fields_ = [("active", C.c_int32), ("load_before", C.c_int32), ("offload_after", C.c_int32),
                 ("reserved", C.c_int32), ("local_step", C.c_int64)]
+
+
+class NormLayer(C.Structure):
+    _fields_ = [("kind", C.c_int32), ("dtype", C.c_int32), ("T", C.c_int64), ("n", C.c_int64), ("X", C.c_void_p),
+                ("ldx", C.c_int64), ("w", C.c_void_p), ("b", C.c_void_p), ("eps", C.c_double)]
+
+
+class LinearLayer(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("activation", C.c_int32), ("out", C.c_int64), ("n_in", C.c_int64),
+                ("T", C.c_int64), ("X", C.c_void_p), ("ldx", C.c_int64), ("W", C.c_void_p), ("ldw", C.c_int64),
+                ("bias", C.c_void_p), ("residual", C.c_void_p), ("ldr", C.c_int64)]
+
+
+class MuonHparams(C.Structure):
+    _fields_ = [("lr", C.c_double), ("momentum", C.c_double), ("weight_decay", C.c_double), ("eps", C.c_double),
+                ("scale", C.c_double), ("steps", C.c_int32), ("nesterov", C.c_int32), ("precision", C.c_int32),
+                ("reserved", C.c_int32)]
 
 
 class ChunkFTError(RuntimeError):
@@ -185,6 +207,25 @@ def _load(path) -> C.CDLL:
     L.chunkft_calib_mfma_bf16.restype = C.c_int
     L.chunkft_calib_mfma_bf16.argtypes = [C.c_int32, C.c_int32, C.c_void_p, C.c_size_t, C.POINTER(C.c_double),
                                           C.POINTER(C.c_double), C.c_void_p]
+    V, I, N = C.c_void_p, C.c_int64, C.c_size_t
+    L.chunkft_norm_forward.restype = C.c_int
+    L.chunkft_norm_forward.argtypes = [C.POINTER(NormLayer), V, I, V, V]
+    L.chunkft_norm_workspace_bytes.restype = N
+    L.chunkft_norm_workspace_bytes.argtypes = [C.POINTER(NormLayer)]
+    L.chunkft_norm_backward.restype = C.c_int
+    L.chunkft_norm_backward.argtypes = [C.POINTER(NormLayer), V, V, I, V, I, V, I, I, V, I, I, C.c_int, V, N, V]
+    L.chunkft_linear_workspace_bytes.restype = N
+    L.chunkft_linear_workspace_bytes.argtypes = [C.POINTER(LinearLayer), C.c_int]
+    L.chunkft_linear_forward.restype = C.c_int
+    L.chunkft_linear_forward.argtypes = [C.POINTER(LinearLayer), V, I, V, I, V, N, V]
+    L.chunkft_linear_backward.restype = C.c_int
+    L.chunkft_linear_backward.argtypes = [C.POINTER(LinearLayer), V, I, V, I, V, I, V, I, V, I, I, C.c_int, V, N, V]
+    L.chunkft_orthogonalize_workspace_bytes.restype = N
+    L.chunkft_orthogonalize_workspace_bytes.argtypes = [C.c_int32, I, I]
+    L.chunkft_orthogonalize.restype = C.c_int
+    L.chunkft_orthogonalize.argtypes = [V, I, C.c_int32, I, I, C.c_int32, C.c_double, V, I, V, N, V]
+    L.chunkft_muon_chunk.restype = C.c_int
+    L.chunkft_muon_chunk.argtypes = [V, V, V, V, C.c_int32, I, I, C.POINTER(MuonHparams), V, N, V]
     return L
 
 
@@ -193,7 +234,9 @@ EXPORTS = ("chunkft_plan_cycle", "chunkft_plan_stats", "chunkft_split_k", "chunk
            "chunkft_wgrad_adamw_fused_group", "chunkft_group_workspace_bytes", "chunkft_status_string",
            "chunkft_version", "chunkft_calib_mfma_bf16", "chunkft_calib_mfma_bf16_shape", "chunkft_schedule_at",
            "chunkft_mover_create", "chunkft_mover_destroy", "chunkft_mover_load", "chunkft_mover_await_load",
-           "chunkft_mover_offload", "chunkft_mover_sync")
+           "chunkft_mover_offload", "chunkft_mover_sync", "chunkft_norm_forward", "chunkft_norm_workspace_bytes",
+           "chunkft_norm_backward", "chunkft_linear_workspace_bytes", "chunkft_linear_forward", "chunkft_linear_backward",
+           "chunkft_orthogonalize_workspace_bytes", "chunkft_orthogonalize", "chunkft_muon_chunk")
 
 
 def status_string(status: int) -> str:
@@ -424,6 +467,197 @@ def chunkft_wgrad_adamw_fused_static(layer: Layer, begin: int, end: int, W, mast
                                                 _ptr(v), C.byref(hp), _stream_ptr(stream))
     if check and st != OK:
         raise ChunkFTError(st, "chunkft_wgrad_adamw_fused_static")
+    return st
+
+
+# ----------------------------------------------------------------- layers
+def _on_device(t, name: str, dtype):
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must be {dtype}")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must live on the GPU")
+    if t.get_device() != _torch.cuda.current_device():
+        raise ValueError(f"{name} must live on the current device")
+
+
+def _rows(t, name: str, width: int, dtype, rows: Optional[int] = None):
+    """(pointer, row stride) of a 2-D device tensor of `width` columns (None: (None, 0))."""
+    if t is None:
+        return None, 0
+    s = t.stride()
+    if len(s) != 2 or t.shape[1] != width or (rows is not None and t.shape[0] != rows):
+        raise ValueError(f"{name} must be [{'tokens' if rows is None else rows}, {width}]")
+    if s[1] != 1 and width != 1:
+        raise ValueError(f"{name} must have unit inner stride")
+    _on_device(t, name, dtype)
+    # the stride of a dimension of one says nothing
+    return t.data_ptr(), s[0] if t.shape[0] != 1 else max(s[0], width)
+
+
+def _vector(t, name: str, n: int, dtype):
+    if t is None:
+        return None
+    if t.dim() != 1 or t.shape[0] != n or (t.stride(0) != 1 and n != 1):
+        raise ValueError(f"{name} must be a contiguous vector of {n} elements")
+    _on_device(t, name, dtype)
+    return t.data_ptr()
+
+
+def _flat(t, name: str, n: int, dtype):
+    """n elements in one piece, of whatever shape."""
+    if t is None:
+        return None
+    if t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{name} must hold {n} contiguous elements")
+    _on_device(t, name, dtype)
+    return t.data_ptr()
+
+
+def _grad_range(g, name: str, span: Optional[Tuple[int, int]], n: int):
+    """(pointer, begin, end) of the fp32 gradient of the elements [begin, end) of a vector (None: all of them)."""
+    if g is None:
+        return None, 0, 0
+    begin, end = (0, n) if span is None else span
+    return _vector(g, name, end - begin, _torch.float32), begin, end
+
+
+def _workspace(ws):
+    if ws is None:
+        return None, 0
+    n = ws.numel()
+    return _flat(ws, "ws", n, ws.dtype), n * ws.element_size()
+
+
+def _dtype_of(layer):
+    return _torch.float32 if layer.dtype == F32 else _torch.bfloat16
+
+
+def make_norm(kind: int, X, w=None, b=None, eps: float = 1e-5) -> NormLayer:
+    """Describe an RMSNORM or LAYERNORM layer over the rows of X [tokens, n]; w, b: n elements of X's dtype or None."""
+    d = _torch_dtype_code(X)
+    if X.dim() != 2:
+        raise ValueError("X must be 2-D")
+    n = X.shape[1]
+    p, ld = _rows(X, "X", n, X.dtype)
+    layer = NormLayer(kind, d, X.shape[0], n, p, ld, _vector(w, "w", n, X.dtype), _vector(b, "b", n, X.dtype), float(eps))
+    layer.tensors = X, w, b                                 # alive as long as the description is
+    return layer
+
+
+def chunkft_norm_workspace_bytes(layer: NormLayer) -> int:
+    return lib().chunkft_norm_workspace_bytes(C.byref(layer))
+
+
+def chunkft_norm_forward(layer: NormLayer, Y, stats=None, stream=None, check: bool = True) -> int:
+    """stats: None or a contiguous fp32 [tokens, 2] tensor (mean and reciprocal deviation of every token)."""
+    p, ld = _rows(Y, "Y", layer.n, _dtype_of(layer), layer.T)
+    st = lib().chunkft_norm_forward(C.byref(layer), p, ld, _stats(stats, layer), _stream_ptr(stream))
+    if check and st != OK:
+        raise ChunkFTError(st, "chunkft_norm_forward")
+    return st
+
+
+def _stats(stats, layer: NormLayer):
+    if stats is None:
+        return None
+    if tuple(stats.shape) != (layer.T, 2):
+        raise ValueError("stats must be [tokens, 2]")
+    return _flat(stats, "stats", 2 * layer.T, _torch.float32)
+
+
+def chunkft_norm_backward(layer: NormLayer, stats, dY, dX=None, dw=None, w_range=None, db=None, b_range=None,
+                          accumulate: bool = False, ws=None, stream=None, check: bool = True) -> int:
+    """w_range, b_range: (begin, end) of the elements that dw and db hold (None: all)."""
+    T, dt = layer.T, _dtype_of(layer)
+    py, ldy = _rows(dY, "dY", layer.n, dt, T)
+    px, ldx = _rows(dX, "dX", layer.n, dt, T)
+    pw, pb = _grad_range(dw, "dw", w_range, layer.n), _grad_range(db, "db", b_range, layer.n)
+    st = lib().chunkft_norm_backward(C.byref(layer), _stats(stats, layer), py, ldy, px, ldx, *pw, *pb, int(accumulate),
+                                     *_workspace(ws), _stream_ptr(stream))
+    if check and st != OK:
+        raise ChunkFTError(st, "chunkft_norm_backward")
+    return st
+
+
+def make_linear(X, W, bias=None, activation: int = ACT_NONE, residual=None, tokens: Optional[int] = None) -> LinearLayer:
+    """Describe y = act(X W^T + bias) + residual with W [out, in].  The backward pass needs no X: pass None and `tokens`."""
+    d = _torch_dtype_code(W)
+    if W.dim() != 2:
+        raise ValueError("W must be 2-D")
+    out, n_in = W.shape
+    pw, ldw = _rows(W, "W", n_in, W.dtype)
+    px, ldx = _rows(X, "X", n_in, W.dtype, tokens)
+    T = X.shape[0] if X is not None else tokens
+    if T is None:
+        raise ValueError("give X or tokens")
+    pr, ldr = _rows(residual, "residual", out, W.dtype, T)
+    layer = LinearLayer(d, activation, out, n_in, T, px, ldx, pw, ldw, _vector(bias, "bias", out, W.dtype), pr, ldr)
+    layer.tensors = X, W, bias, residual                    # alive as long as the description is
+    return layer
+
+
+def chunkft_linear_workspace_bytes(layer: LinearLayer, backward: bool = False) -> int:
+    return lib().chunkft_linear_workspace_bytes(C.byref(layer), int(backward))
+
+
+def chunkft_linear_forward(layer: LinearLayer, Y, Z=None, ws=None, stream=None, check: bool = True) -> int:
+    dt = _dtype_of(layer)
+    st = lib().chunkft_linear_forward(C.byref(layer), *_rows(Y, "Y", layer.out, dt, layer.T), *_rows(Z, "Z", layer.out, dt, layer.T),
+                                      *_workspace(ws), _stream_ptr(stream))
+    if check and st != OK:
+        raise ChunkFTError(st, "chunkft_linear_forward")
+    return st
+
+
+def chunkft_linear_backward(layer: LinearLayer, dY, Z=None, dZ=None, dX=None, db=None, b_range=None, accumulate: bool = False,
+                            ws=None, stream=None, check: bool = True) -> int:
+    """Without an activation Z and dZ are ignored (dz is dY).  b_range: (begin, end) of the elements that db holds (None: all)."""
+    dt, T = _dtype_of(layer), layer.T
+    if layer.activation == ACT_NONE:
+        Z = dZ = None
+    st = lib().chunkft_linear_backward(C.byref(layer), *_rows(dY, "dY", layer.out, dt, T), *_rows(Z, "Z", layer.out, dt, T),
+                                       *_rows(dZ, "dZ", layer.out, dt, T), *_rows(dX, "dX", layer.n_in, dt, T),
+                                       *_grad_range(db, "db", b_range, layer.out), int(accumulate), *_workspace(ws),
+                                       _stream_ptr(stream))
+    if check and st != OK:
+        raise ChunkFTError(st, "chunkft_linear_backward")
+    return st
+
+
+# ---------------------------------------------------- orthogonalised updates
+def chunkft_orthogonalize_workspace_bytes(precision: int, rows: int, cols: int) -> int:
+    return lib().chunkft_orthogonalize_workspace_bytes(precision, rows, cols)
+
+
+def chunkft_orthogonalize(G, O, steps: int = 5, eps: float = 1e-7, ws=None, stream=None, check: bool = True) -> int:
+    """O = Newton-Schulz steps on G, both [rows, cols] of one dtype; O may be G itself."""
+    d = _torch_dtype_code(G)
+    if G.dim() != 2:
+        raise ValueError("G must be 2-D")
+    rows, cols = G.shape
+    pg, ldg = _rows(G, "G", cols, G.dtype)
+    po, ldo = _rows(O, "O", cols, G.dtype, rows)
+    st = lib().chunkft_orthogonalize(pg, ldg, d, rows, cols, steps, eps, po, ldo, *_workspace(ws), _stream_ptr(stream))
+    if check and st != OK:
+        raise ChunkFTError(st, "chunkft_orthogonalize")
+    return st
+
+
+def muon_hparams(lr, momentum=0.95, weight_decay=0.0, eps=1e-7, scale=1.0, steps=5, nesterov=True,
+                 precision: int = F32) -> MuonHparams:
+    return MuonHparams(lr, momentum, weight_decay, eps, scale, steps, int(nesterov), precision, 0)
+
+
+def chunkft_muon_chunk(g, master, m, W_at_begin, rows: int, cols: int, hp: MuonHparams, w_dtype: int = BF16, ws=None,
+                       stream=None, check: bool = True) -> int:
+    """The update of `rows` whole rows of `cols` columns; g, master, m hold rows * cols floats, W_at_begin (or None) the segment's
+    rows * cols elements of the parameter."""
+    torch, n = _torch_module(), rows * cols
+    W = _flat(W_at_begin, "W_at_begin", n, torch.float32 if w_dtype == F32 else torch.bfloat16)
+    st = lib().chunkft_muon_chunk(*[_flat(t, name, n, torch.float32) for t, name in ((g, "g"), (master, "master"), (m, "m"))], W, w_dtype,
+                                  rows, cols, C.byref(hp), *_workspace(ws), _stream_ptr(stream))
+    if check and st != OK:
+        raise ChunkFTError(st, "chunkft_muon_chunk")
     return st
 
 

@@ -1,0 +1,98 @@
+// Internal interface between the C ABI of the layer and update operators (layers_api.cpp) and their kernels.
+#ifndef CHUNKFT_LAYERS_H
+#define CHUNKFT_LAYERS_H
+
+#include <cstddef>
+#include <cstdint>
+
+namespace chunkft {
+
+// ------------------------------------------------------------------ norm layer (norm.hip)
+struct NormProblem {
+  const void* X;
+  const void* w;       // scale, or nullptr (ones)
+  const void* b;       // shift, or nullptr (zeros)
+  int64_t ldx, T, n;
+  float eps;
+  bool subtract_mean;
+};
+
+struct NormGrads {
+  const float* stats;  // [T][2]
+  const void* dY;
+  void* dX;            // or nullptr
+  int64_t lddy, lddx;
+  float* dw;           // columns [w0, w1) at dw[0 ..], or nullptr
+  float* db;
+  int64_t w0, w1, b0, b1;
+  int accumulate;
+};
+
+// Workgroups that a backward pass leaves partial sums of the vectors' gradients from; each leaves two rows of norm_pitch floats.
+int64_t norm_parts(int64_t T, int64_t n, int dtype, int compute_units);
+inline int64_t norm_pitch(int64_t n) { return (n + 31) / 32 * 32; }
+
+int launch_norm_forward(const NormProblem& p, int dtype, void* Y, int64_t ldy, float* stats, void* stream);
+int launch_norm_backward(const NormProblem& p, int dtype, const NormGrads& g, float* ws, void* stream);
+
+// out[i] (+)= sum over parts, in ascending order within a fixed tree, of ws[part * stride + first + i].
+int launch_sum_parts(const float* ws, int64_t parts, int64_t stride, int64_t first, int64_t count, float* out, int accumulate,
+                     void* stream);
+
+// ---------------------------------------------------------------- linear layer (linear.hip)
+enum Act : int { ACT_NONE = 0, ACT_RELU = 1, ACT_GELU = 2, ACT_SILU = 3 };
+
+struct LinearProblem {
+  const void* X;
+  const void* W;
+  const void* bias;      // or nullptr
+  const void* residual;  // or nullptr
+  int64_t ldx, ldw, ldr, out, in, T;
+  int32_t dtype, act;
+};
+
+struct LinearGrads {
+  const void* dY;
+  const void* Z;         // nullptr without an activation
+  void* dZ;              // nullptr without an activation
+  void* dX;              // or nullptr
+  int64_t lddy, ldz, lddz, lddx;
+  float* db;             // columns [b0, b1), or nullptr
+  int64_t b0, b1;
+  int accumulate;
+};
+
+// Rows of partial sums (of norm_pitch(out) floats) that a backward pass leaves for the bias.
+int64_t linear_parts(int64_t T, int64_t out, int dtype, int compute_units);
+
+int launch_linear_forward(const LinearProblem& p, void* Y, int64_t ldy, void* Z, int64_t ldz, void* stream);
+int launch_linear_backward(const LinearProblem& p, const LinearGrads& g, float* ws, void* stream);
+
+// ------------------------------------------------------- orthogonalised update (orthogonalize.hip)
+struct OrthoProblem {
+  int64_t rows, cols;
+  int32_t planes;        // 1: 16-bit operands, 2: 22-bit operands
+  int32_t steps;
+  float eps;
+  // what is orthogonalised: G (bf16 or fp32), or the momentum step on g and m
+  const void* G;
+  int64_t ldg;
+  int32_t g_dtype;
+  float* m;              // nullptr: G itself
+  float momentum;
+  bool nesterov;
+  // where it goes: O, or the update
+  void* O;
+  int64_t ldo;
+  int32_t o_dtype;
+  float* master;         // nullptr: O
+  void* W;
+  int32_t w_kind;        // WKind
+  float lr, scale, weight_decay;
+};
+
+size_t ortho_workspace_bytes(int64_t rows, int64_t cols, int planes);
+int launch_orthogonalize(const OrthoProblem& p, void* ws, void* stream);
+
+}  // namespace chunkft
+#endif
