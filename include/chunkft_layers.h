@@ -100,7 +100,7 @@ int chunkft_linear_forward(const chunkft_linear* L, void* Y, int64_t ldy, void* 
  * dX (device, out) NULL or [T, in].
  * db (device, out) NULL, or the fp32 gradient of the elements [b_begin, b_end) of the bias, element b_begin + i at index i, summed
  *   before dz is rounded; accumulate as in chunkft_norm_backward.
- * ws  may be NULL when db is; 16-byte aligned.
+ * ws  may be NULL when the call needs none; 16-byte aligned.  chunkft_linear_workspace_bytes covers every combination of outputs.
  * At least one of dZ, dX, db.  Errors: as above, RANGE. */
 int chunkft_linear_backward(const chunkft_linear* L, const void* dY, int64_t lddy, const void* Z, int64_t ldz, void* dZ, int64_t lddz,
                             void* dX, int64_t lddx, float* db, int64_t b_begin, int64_t b_end, int accumulate,

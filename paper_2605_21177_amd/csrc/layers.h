@@ -65,7 +65,16 @@ struct LinearGrads {
 // Rows of partial sums (of norm_pitch(out) floats) that a backward pass leaves for the bias.
 int64_t linear_parts(int64_t T, int64_t out, int dtype, int compute_units);
 
-int launch_linear_forward(const LinearProblem& p, void* Y, int64_t ldy, void* Z, int64_t ldz, void* stream);
+// How a product [M, K] x [K, N] is cut: square tiles of `tile`, `slabs` runs of kslab values of k.  From the shape alone: the workspace
+// that the caller gives depends on it.
+struct LinearPlan {
+  int32_t tile, slabs;
+  int64_t kslab;
+};
+LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, int dtype, int compute_units);
+bool linear_takes_few(int64_t T);        // the forward pass reads the weights once, whatever the plan
+
+int launch_linear_forward(const LinearProblem& p, void* Y, int64_t ldy, void* Z, int64_t ldz, float* ws, void* stream);
 int launch_linear_backward(const LinearProblem& p, const LinearGrads& g, float* ws, void* stream);
 
 // ------------------------------------------------------- orthogonalised update (orthogonalize.hip)

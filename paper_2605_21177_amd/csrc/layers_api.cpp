@@ -68,9 +68,19 @@ int check_linear(const chunkft_linear* L, LinearProblem* p) {
   return CHUNKFT_OK;
 }
 
-size_t linear_need(const LinearProblem& p, bool backward) {
-  if (!backward) return 0;
-  return static_cast<size_t>(linear_parts(p.T, p.out, p.dtype, device_compute_units())) * static_cast<size_t>(norm_pitch(p.out)) * 4u;
+// Sums of slabs of a product, rows of `N` padded columns.
+size_t slab_need(int64_t M, int64_t N, int64_t K, int32_t dtype) {
+  const LinearPlan plan = linear_plan(M, N, K, dtype, device_compute_units());
+  return plan.slabs <= 1 ? 0 : static_cast<size_t>(plan.slabs) * static_cast<size_t>(M) * static_cast<size_t>(norm_pitch(N)) * 4u;
+}
+
+size_t forward_need(const LinearProblem& p) { return linear_takes_few(p.T) ? 0 : slab_need(p.T, p.out, p.in, p.dtype); }
+
+// The bias' partial sums are done with when the product's begin: one after the other on the stream they share the space.
+size_t backward_need(const LinearProblem& p, bool bias, bool input) {
+  const size_t sums = bias ? static_cast<size_t>(linear_parts(p.T, p.out, p.dtype, device_compute_units())) * static_cast<size_t>(norm_pitch(p.out)) * 4u : 0;
+  const size_t slabs = input ? slab_need(p.T, p.in, p.out, p.dtype) : 0;
+  return sums > slabs ? sums : slabs;
 }
 
 bool matrix_ok(int64_t rows, int64_t cols) {
@@ -116,7 +126,8 @@ extern "C" int chunkft_norm_backward(const chunkft_norm* N, const float* stats, 
 
 extern "C" size_t chunkft_linear_workspace_bytes(const chunkft_linear* L, int backward) {
   LinearProblem p;
-  return check_linear(L, &p) == CHUNKFT_OK ? linear_need(p, backward != 0) : 0;
+  if (check_linear(L, &p) != CHUNKFT_OK) return 0;
+  return backward ? backward_need(p, true, true) : forward_need(p);
 }
 
 extern "C" int chunkft_linear_forward(const chunkft_linear* L, void* Y, int64_t ldy, void* Z, int64_t ldz, void* ws, size_t ws_bytes,
@@ -131,9 +142,9 @@ extern "C" int chunkft_linear_forward(const chunkft_linear* L, void* Y, int64_t 
   if (s == CHUNKFT_OK && Z) s = check_rows(Z, p.T, p.out, ldz, es);
   if (s == CHUNKFT_OK && p.bias && !aligned(p.bias, es)) s = CHUNKFT_ERR_INVALID_ARG;
   if (s == CHUNKFT_OK && p.residual == Y && p.ldr != ldy) s = CHUNKFT_ERR_INVALID_ARG;
-  if (s == CHUNKFT_OK) s = check_workspace(ws, ws_bytes, linear_need(p, false), 16);
+  if (s == CHUNKFT_OK) s = check_workspace(ws, ws_bytes, forward_need(p), 16);
   if (s != CHUNKFT_OK) return s;
-  return done(launch_linear_forward(p, Y, ldy, Z, ldz, stream));
+  return done(launch_linear_forward(p, Y, ldy, Z, ldz, static_cast<float*>(ws), stream));
 }
 
 extern "C" int chunkft_linear_backward(const chunkft_linear* L, const void* dY, int64_t lddy, const void* Z, int64_t ldz, void* dZ,
@@ -151,7 +162,7 @@ extern "C" int chunkft_linear_backward(const chunkft_linear* L, const void* dY, 
   if (s == CHUNKFT_OK && act) s = check_rows(dZ, p.T, p.out, lddz, es);
   if (s == CHUNKFT_OK && dX) s = check_rows(dX, p.T, p.in, lddx, es);
   if (s == CHUNKFT_OK) s = check_range(db, b_begin, b_end, p.out);
-  if (s == CHUNKFT_OK) s = check_workspace(ws, ws_bytes, db ? linear_need(p, true) : 0, 16);
+  if (s == CHUNKFT_OK) s = check_workspace(ws, ws_bytes, backward_need(p, db != nullptr, dX != nullptr), 16);
   if (s != CHUNKFT_OK) return s;
   const LinearGrads g{dY, Z, dZ, dX, lddy, ldz, lddz, lddx, db, b_begin, b_end, accumulate};
   return done(launch_linear_backward(p, g, static_cast<float*>(ws), stream));

@@ -6,6 +6,8 @@
 //   dx = dz W                          the product with W across k
 #include <hip/hip_runtime.h>
 
+#include <cmath>
+
 #include "internal.h"
 #include "launch.h"
 #include "layers.h"
@@ -67,32 +69,167 @@ __device__ __forceinline__ void finish_row(const Epilogue& e, int64_t m, int64_t
   x.store((T*)e.Y + m * e.ldy + n, valid);
 }
 
-template <class C, int KB, bool DMA>
-__global__ __launch_bounds__(C::NT, C::MINW) void linear_kernel(const Product q, const TileOrder o, int n_items, const Epilogue e) {
+// A product whose sum over k is cut into slabs of kslab leaves the sums of each in ws, slab by slab, rows of `pitch` floats.
+struct Slabs {
+  int64_t kslab, pitch;
+  float* ws;
+  int32_t count;
+};
+
+// Slab `slab` of a product: a product over fewer k.
+template <class P, int KB>
+__device__ __forceinline__ P slab_of(P q, const Slabs& s, int slab) {
+  const int64_t k0 = slab * s.kslab;
+  q.A += k0;
+  q.B += KB ? k0 * q.ldb : k0;
+  q.K = q.K - k0 < s.kslab ? q.K - k0 : s.kslab;
+  return q;
+}
+
+template <class C, int KB, bool DMA, bool SPLIT>
+__global__ __launch_bounds__(C::NT, C::MINW) void linear_kernel(const Product whole, const TileOrder o, int n_items, const Epilogue e,
+                                                                const Slabs s) {
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
   const int item = xcd_work_item(n_items);
   if (item < 0) return;
+  const int tiles = o.tiles_m * o.tiles_n, slab = SPLIT ? item / tiles : 0;
   int tm, tn;
-  tile_at(o, item, tm, tn);
+  tile_at(o, item - slab * tiles, tm, tn);
+  const Product q = SPLIT ? slab_of<Product, KB>(whole, s, slab) : whole;
   const int64_t row0 = (int64_t)tm * C::BM, col0 = (int64_t)tn * C::BN;
   product_tile<C, 0, KB, false, DMA>(q, row0, col0, lds, [&](int m, int n, float (&v)[8]) {
-    if (row0 + m < q.M && col0 + n < q.N) finish_row<unsigned short>(e, row0 + m, col0 + n, q.N - col0 - n, v);
+    const int64_t r = row0 + m, c = col0 + n;
+    if (r >= q.M || c >= q.N) return;
+    if constexpr (SPLIT) {                        // the pitch is a multiple of 8: whole pieces
+      float* const p = s.ws + (slab * q.M + r) * s.pitch + c;
+      *(f32x4*)p = *(const f32x4*)v;
+      *(f32x4*)(p + 4) = *(const f32x4*)(v + 4);
+    } else {
+      finish_row<unsigned short>(e, r, c, q.N - c, v);
+    }
   });
 }
 
-template <int BM, int BN, int KB>
-__global__ __launch_bounds__(256, 2) void linear_f32_kernel(const ProductF32 q, const TileOrder o, int n_items, const Epilogue e) {
+template <int BM, int BN, int KB, bool SPLIT>
+__global__ __launch_bounds__(256, 2) void linear_f32_kernel(const ProductF32 whole, const TileOrder o, int n_items, const Epilogue e,
+                                                            const Slabs s) {
   __shared__ __attribute__((aligned(16))) float lds[F32Cfg<BM, BN, 2, 2>::LDS / 4];
   const int item = xcd_work_item(n_items);
   if (item < 0) return;
+  const int tiles = o.tiles_m * o.tiles_n, slab = SPLIT ? item / tiles : 0;
   int tm, tn;
-  tile_at(o, item, tm, tn);
+  tile_at(o, item - slab * tiles, tm, tn);
+  const ProductF32 q = SPLIT ? slab_of<ProductF32, KB>(whole, s, slab) : whole;
   const int64_t row0 = (int64_t)tm * BM, col0 = (int64_t)tn * BN;
   product_tile_f32<BM, BN, 2, 2, KB>(q, row0, col0, lds, [&](int m, int n, const f32x4& x) {
-    if (row0 + m >= q.M || col0 + n >= q.N) return;
-    float v[4] = {x[0], x[1], x[2], x[3]};
-    finish_row<float>(e, row0 + m, col0 + n, q.N - col0 - n, v);
+    const int64_t r = row0 + m, c = col0 + n;
+    if (r >= q.M || c >= q.N) return;
+    if constexpr (SPLIT) {
+      *(f32x4*)(s.ws + (slab * q.M + r) * s.pitch + c) = x;
+    } else {
+      float v[4] = {x[0], x[1], x[2], x[3]};
+      finish_row<float>(e, r, c, q.N - c, v);
+    }
   });
+}
+
+// The slabs' sums, added in order, through the epilogue: a piece of a row per lane.
+template <typename T>
+__global__ __launch_bounds__(256) void join_slabs_kernel(const Slabs s, int64_t M, int64_t N, const Epilogue e) {
+  constexpr int VE = Row<T>::N;
+  const int64_t per_row = (N + VE - 1) / VE, n = M * per_row;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+    const int64_t r = i / per_row, c = i % per_row * VE;
+    float v[VE];
+#pragma unroll
+    for (int h = 0; h < VE; h += 4) *(f32x4*)(v + h) = *(const f32x4*)(s.ws + r * s.pitch + c + h);
+    for (int k = 1; k < s.count; ++k) {
+#pragma unroll
+      for (int h = 0; h < VE; h += 4) {
+        const f32x4 x = *(const f32x4*)(s.ws + (k * M + r) * s.pitch + c + h);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) v[h + u] += x[u];
+      }
+    }
+    finish_row<T>(e, r, c, N - c, v);
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ few tokens
+// Up to 16 NB tokens: the weights are read once and nothing else counts.  A workgroup has 16 rows of W; its eight waves take pieces
+// of 128 bytes of them in turn, straight from memory into the registers of the matrix instruction (a lane has 16 bytes of one
+// row), against the same k of x, which stay in the caches.  The eight sums meet in LDS, in order.
+template <typename T> struct FewStep;
+template <> struct FewStep<unsigned short> {
+  static constexpr int K = 32;                   // of an instruction group
+  __device__ __forceinline__ static f32x4 mul(const Row<unsigned short>& w, const Row<unsigned short>& x, f32x4 c) {
+    return mfma16<false>(__builtin_bit_cast(s16x8, w.v), __builtin_bit_cast(s16x8, x.v), c);
+  }
+};
+template <> struct FewStep<float> {
+  static constexpr int K = 16;                   // a lane's four k go to four instructions
+  __device__ __forceinline__ static f32x4 mul(const Row<float>& w, const Row<float>& x, f32x4 c) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(w.v[j], x.v[j], c, 0, 0, 0);
+    return c;
+  }
+};
+
+constexpr int kFewWaves = 8, kFewUnroll = 4;
+template <typename T, int NB>
+__global__ __launch_bounds__(64 * kFewWaves) void linear_few_kernel(const T* X, int64_t ldx, const T* W, int64_t ldw, int64_t tokens,
+                                                                    int64_t out, int64_t n_in, const Epilogue e) {
+  constexpr int VE = Row<T>::N, KS = FewStep<T>::K, STEP = KS * kFewUnroll, PITCH = 20;
+  __shared__ __attribute__((aligned(16))) float part[kFewWaves][NB * 16][PITCH];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i16 = lane & 15, g = lane >> 4;
+  const int64_t row0 = (int64_t)blockIdx.x * 16, row = row0 + i16;
+  const T* const w = W + (row < out ? row : out - 1) * ldw + g * VE;
+  f32x4 acc[NB];
+#pragma unroll
+  for (int b = 0; b < NB; ++b) acc[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+  int64_t k = (int64_t)wave * STEP;
+  for (; k + STEP <= n_in; k += kFewWaves * STEP) {
+    Row<T> wr[kFewUnroll], xr[NB][kFewUnroll];
+#pragma unroll
+    for (int u = 0; u < kFewUnroll; ++u) wr[u].load(w + k + u * KS, VE);
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      const int64_t t = b * 16 + i16;
+#pragma unroll
+      for (int u = 0; u < kFewUnroll; ++u) xr[b][u].load(X + (t < tokens ? t : 0) * ldx + g * VE + k + u * KS, VE);
+    }
+#pragma unroll
+    for (int u = 0; u < kFewUnroll; ++u)
+#pragma unroll
+      for (int b = 0; b < NB; ++b) acc[b] = FewStep<T>::mul(wr[u], xr[b][u], acc[b]);
+  }
+  for (; k < n_in; k += KS) {                    // the one wave whose piece the end of the rows cuts
+    const int64_t left = n_in - k - g * VE;
+    Row<T> wr, xr;
+    wr.load(w + k, left);
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      const int64_t t = b * 16 + i16;
+      xr.load(X + (t < tokens ? t : 0) * ldx + g * VE + k, left);
+      acc[b] = FewStep<T>::mul(wr, xr, acc[b]);
+    }
+  }
+#pragma unroll
+  for (int b = 0; b < NB; ++b) *(f32x4*)&part[wave][b * 16 + i16][g * 4] = acc[b];
+  __syncthreads();
+  constexpr int PPR = 16 / VE;                   // pieces of a token's 16 results
+  for (int i = threadIdx.x; i < NB * 16 * PPR; i += 64 * kFewWaves) {
+    const int t = i / PPR, c = i % PPR * VE;
+    if (t >= tokens || row0 + c >= out) continue;
+    float v[VE];
+#pragma unroll
+    for (int u = 0; u < VE; ++u) {
+      v[u] = part[0][t][c + u];
+#pragma unroll
+      for (int q = 1; q < kFewWaves; ++q) v[u] += part[q][t][c + u];
+    }
+    finish_row<T>(e, t, row0 + c, out - row0 - c, v);
+  }
 }
 
 // --------------------------------------------------------------------- dz = dy act'(z) and its sums over the tokens
@@ -154,46 +291,75 @@ int launch_gate(const LinearProblem& p, const LinearGrads& g, float* ws, hipStre
 }
 
 // ------------------------------------------------------------------------------------------------------- launches
-bool fill_order(int64_t M, int64_t N, int64_t bm, int64_t bn, int threads, TileOrder& o, int& n_items) {
+bool fill_order(int64_t M, int64_t N, int64_t bm, int64_t bn, int threads, int slabs, TileOrder& o, int& n_items) {
   const int64_t tm = ceil_div(M, bm), tn = ceil_div(N, bn);
-  if (tm > 0x3fffffff || tn > 0x3fffffff || tm * tn > kMaxLaunchThreads / threads - 8 || tm * tn > 0x3fffffff) return false;
+  if (tm > 0x3fffffff || tn > 0x3fffffff || tm * tn > kMaxLaunchThreads / threads / slabs - 8 || tm * tn > 0x3fffffff / slabs) return false;
   o = TileOrder{(int)tm, (int)tn, 8};
-  n_items = (int)(tm * tn);
+  n_items = (int)(tm * tn * slabs);
   return true;
 }
 
-typedef ProductCfg<128, 128, 64, 2, 2, 2> Tile128;
+typedef ProductCfg<256, 256, 64, 4, 2, 3, 2> Tile256;
+typedef ProductCfg<128, 128, 64, 2, 2, 2, 2> Tile128;
 
-template <class C, int KB, bool DMA>
-int launch_tiles(const Product& q, const Epilogue& e, hipStream_t st) {
+template <class C, int KB, bool DMA, bool SPLIT>
+int launch_tiles(const Product& q, const Epilogue& e, const Slabs& s, hipStream_t st) {
   TileOrder o;
   int n;
-  if (!fill_order(q.M, q.N, C::BM, C::BN, C::NT, o, n)) return (int)hipErrorInvalidValue;
-  const int err = raise_lds_limit<linear_kernel<C, KB, DMA>>(C::LDS);
+  if (!fill_order(q.M, q.N, C::BM, C::BN, C::NT, s.count, o, n)) return (int)hipErrorInvalidValue;
+  const int err = raise_lds_limit<linear_kernel<C, KB, DMA, SPLIT>>(C::LDS);
   if (err != 0) return err;
-  hipLaunchKernelGGL((linear_kernel<C, KB, DMA>), dim3((unsigned)((n + 7) / 8 * 8)), dim3(C::NT), C::LDS, st, q, o, n, e);
+  hipLaunchKernelGGL((linear_kernel<C, KB, DMA, SPLIT>), dim3((unsigned)((n + 7) / 8 * 8)), dim3(C::NT), C::LDS, st, q, o, n, e, s);
   return (int)hipGetLastError();
 }
 
-template <int BM, int BN, int KB>
-int launch_tiles_f32(const ProductF32& q, const Epilogue& e, hipStream_t st) {
+template <int BM, int BN, int KB, bool SPLIT>
+int launch_tiles_f32(const ProductF32& q, const Epilogue& e, const Slabs& s, hipStream_t st) {
   TileOrder o;
   int n;
-  if (!fill_order(q.M, q.N, BM, BN, 256, o, n)) return (int)hipErrorInvalidValue;
-  hipLaunchKernelGGL((linear_f32_kernel<BM, BN, KB>), dim3((unsigned)((n + 7) / 8 * 8)), dim3(256), 0, st, q, o, n, e);
+  if (!fill_order(q.M, q.N, BM, BN, 256, s.count, o, n)) return (int)hipErrorInvalidValue;
+  hipLaunchKernelGGL((linear_f32_kernel<BM, BN, KB, SPLIT>), dim3((unsigned)((n + 7) / 8 * 8)), dim3(256), 0, st, q, o, n, e, s);
+  return (int)hipGetLastError();
+}
+
+template <typename T>
+int join_slabs(const Slabs& s, int64_t M, int64_t N, const Epilogue& e, hipStream_t st) {
+  const int64_t blocks = ceil_div(M * ceil_div(N, Row<T>::N), 256);
+  hipLaunchKernelGGL((join_slabs_kernel<T>), dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(256), 0, st, s, M, N, e);
   return (int)hipGetLastError();
 }
 
 template <int KB>
 int launch_product(const void* A, int64_t lda, const void* B, int64_t ldb, int64_t M, int64_t N, int64_t K, int dtype, const Epilogue& e,
-                   hipStream_t st) {
+                   float* ws, hipStream_t st) {
+  const LinearPlan plan = linear_plan(M, N, K, dtype, device_compute_units());
+  const Slabs s{plan.kslab, norm_pitch(N), ws, plan.slabs};
+  int err;
   if (dtype == 0) {
     const ProductF32 q{(const float*)A, (const float*)B, lda, ldb, M, N, K};
-    return launch_tiles_f32<64, 64, KB>(q, e, st);
+    if (plan.slabs > 1) err = plan.tile == 128 ? launch_tiles_f32<128, 128, KB, true>(q, e, s, st) : launch_tiles_f32<64, 64, KB, true>(q, e, s, st);
+    else err = plan.tile == 128 ? launch_tiles_f32<128, 128, KB, false>(q, e, s, st) : launch_tiles_f32<64, 64, KB, false>(q, e, s, st);
+    return err != 0 || plan.slabs == 1 ? err : join_slabs<float>(s, M, N, e, st);
   }
   const Product q{(const unsigned short*)A, (const unsigned short*)B, lda, ldb, 0, 0, M, N, K};
-  if (direct_rows(A, lda, K, false) && direct_rows(B, ldb, N, KB != 0)) return launch_tiles<Tile128, KB, true>(q, e, st);
-  return launch_tiles<Tile128, KB, false>(q, e, st);
+  const bool direct = direct_rows(A, lda, K, false) && direct_rows(B, ldb, N, KB != 0);
+  if (plan.slabs > 1) {
+    if (!direct) err = launch_tiles<Tile128, KB, false, true>(q, e, s, st);
+    else err = plan.tile == 256 ? launch_tiles<Tile256, KB, true, true>(q, e, s, st) : launch_tiles<Tile128, KB, true, true>(q, e, s, st);
+    return err != 0 ? err : join_slabs<unsigned short>(s, M, N, e, st);
+  }
+  if (!direct) return launch_tiles<Tile128, KB, false, false>(q, e, s, st);
+  return plan.tile == 256 ? launch_tiles<Tile256, KB, true, false>(q, e, s, st) : launch_tiles<Tile128, KB, true, false>(q, e, s, st);
+}
+
+template <typename T>
+int launch_few(const LinearProblem& p, const Epilogue& e, hipStream_t st) {
+  const int64_t blocks = ceil_div(p.out, 16);
+  if (blocks > kMaxLaunchThreads / (64 * kFewWaves)) return (int)hipErrorInvalidValue;
+  const dim3 grid((unsigned)blocks), threads(64 * kFewWaves);
+  if (p.T <= 16) hipLaunchKernelGGL((linear_few_kernel<T, 1>), grid, threads, 0, st, (const T*)p.X, p.ldx, (const T*)p.W, p.ldw, p.T, p.out, p.in, e);
+  else hipLaunchKernelGGL((linear_few_kernel<T, 2>), grid, threads, 0, st, (const T*)p.X, p.ldx, (const T*)p.W, p.ldw, p.T, p.out, p.in, e);
+  return (int)hipGetLastError();
 }
 
 }  // namespace
@@ -204,9 +370,57 @@ int64_t linear_parts(int64_t T, int64_t out, int dtype, int compute_units) {
   return want < 1 ? 1 : want < need ? want : need;
 }
 
-int launch_linear_forward(const LinearProblem& p, void* Y, int64_t ldy, void* Z, int64_t ldz, void* stream) {
+// What a cut costs, in us, from rounds of workgroups (n items of a tile with ks values of k each on so many compute units) and the
+// slabs' traffic.  Measured per 1024 k (and 1 - 2 us around them): bf16, 256-wide tiles, one to a unit, 19.5 where few units have
+// one and 24 where all have; 128-wide ones 10.2 alone on a unit, 14.5 the pair.  fp32: 22 and 18.2 for 64-wide ones alone and
+// each of several, 72 and 64.5 for 128-wide ones.  Slabs: 8 bytes per slab and element at 7 TB/s, and a launch.
+// E.g. bf16, 4096 x 4096 x 14336: 256-wide tiles 388 us, 128-wide 419; 512 x 14336 x 4096 one slab of 128-wide tiles 146, four 64;
+// 1024 x 14336 x 4096 162 and, four slabs of 256-wide tiles, 108.
+double round_cost(int dtype, int tile, double items, double ks, double units) {
+  const double k = ks / 1024;
+  if (dtype == 0) {
+    const double each = std::ceil(items / units);
+    return tile == 64 ? (each <= 1 ? 22 : 18.2 * each) * k : (each <= 1 ? 72 : 64.5 * each) * k;
+  }
+  if (tile == 256) {
+    const double full = std::floor(items / units), rest = items / units - full;
+    return full * (24 * k + 2) + (rest > 0 ? (19.5 + 4.5 * rest) * k + 2 : 0);
+  }
+  const double full = std::floor(items / (2 * units)), rest = items - full * 2 * units;
+  return full * (14.5 * k + 1) + (rest > units ? 14.5 * k + 1 : rest > 0 ? 10.2 * k + 1 : 0);
+}
+
+LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, int dtype, int compute_units) {
+  const int small = dtype == 0 ? 64 : 128;
+  const int64_t unit = dtype == 0 ? 32 : 64;                 // k of a stage: slabs are whole stages
+  // rows without 16-byte pieces go through registers, in small tiles (fp32 always does)
+  const bool direct = K % 8 == 0 && N % 8 == 0;
+  LinearPlan best{small, 1, K};
+  double least = -1;
+  for (int tile = small; tile <= (direct || dtype == 0 ? 2 * small : small); tile *= 2) {
+    const double tiles = (double)ceil_div(M, tile) * (double)ceil_div(N, tile);
+    for (int want = 1; want <= 16; ++want) {
+      const int64_t ks = ceil_div(ceil_div(K, want), unit) * unit;
+      const int64_t slabs = ceil_div(K, ks);
+      if (slabs != want || (want > 1 && ks < 256)) continue;
+      double cost = round_cost(dtype, tile, tiles * (double)slabs, (double)ks, compute_units);
+      if (!direct && dtype != 0) cost *= 1.6;                // 1001 x 2907 x 2705: 51 us where the direct loads' rule says 32
+      if (slabs > 1) cost += 3 + (8.0 * (double)slabs + 4) * (double)M * (double)N / 7e6;
+      if (least < 0 || cost < least) {
+        least = cost;
+        best = LinearPlan{tile, (int32_t)slabs, slabs > 1 ? ks : K};
+      }
+    }
+  }
+  return best;
+}
+bool linear_takes_few(int64_t T) { return T <= 32; }
+
+int launch_linear_forward(const LinearProblem& p, void* Y, int64_t ldy, void* Z, int64_t ldz, float* ws, void* stream) {
+  hipStream_t st = (hipStream_t)stream;
   const Epilogue e{p.bias, p.residual, Y, Z, p.ldr, ldy, ldz, p.act};
-  return launch_product<0>(p.X, p.ldx, p.W, p.ldw, p.T, p.out, p.in, p.dtype, e, (hipStream_t)stream);
+  if (linear_takes_few(p.T)) return p.dtype == 0 ? launch_few<float>(p, e, st) : launch_few<unsigned short>(p, e, st);
+  return launch_product<0>(p.X, p.ldx, p.W, p.ldw, p.T, p.out, p.in, p.dtype, e, ws, st);
 }
 
 int launch_linear_backward(const LinearProblem& p, const LinearGrads& g, float* ws, void* stream) {
@@ -215,7 +429,7 @@ int launch_linear_backward(const LinearProblem& p, const LinearGrads& g, float* 
   if (g.dZ || g.db) err = p.dtype == 0 ? launch_gate<float>(p, g, ws, st) : launch_gate<unsigned short>(p, g, ws, st);
   if (err != 0 || !g.dX) return err;
   const Epilogue e{nullptr, nullptr, g.dX, nullptr, 0, g.lddx, 0, ACT_NONE};
-  return launch_product<1>(g.dZ ? g.dZ : g.dY, g.dZ ? g.lddz : g.lddy, p.W, p.ldw, p.T, p.in, p.out, p.dtype, e, st);
+  return launch_product<1>(g.dZ ? g.dZ : g.dY, g.dZ ? g.lddz : g.lddy, p.W, p.ldw, p.T, p.in, p.out, p.dtype, e, ws, st);
 }
 
 }  // namespace chunkft

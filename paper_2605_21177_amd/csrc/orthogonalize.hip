@@ -335,8 +335,8 @@ int run_steps(const OrthoProblem& p, const Layout& l, const Scalars* sc, unsigne
   return err;
 }
 
-typedef ProductCfg<128, 128, 64, 2, 2, 2, 1> OnePlane;
-typedef ProductCfg<128, 128, 32, 2, 2, 2, 2> TwoPlanes;
+typedef ProductCfg<128, 128, 64, 2, 2, 2, 2, 1> OnePlane;
+typedef ProductCfg<128, 128, 32, 2, 2, 2, 2, 2> TwoPlanes;
 
 template <typename T>
 int prepare_planes(const OrthoProblem& p, const Layout& l, double* parts, Scalars* sc, unsigned short* x, hipStream_t st) {
