@@ -35,8 +35,12 @@ inline int64_t norm_pitch(int64_t n) { return (n + 31) / 32 * 32; }
 int launch_norm_forward(const NormProblem& p, int dtype, void* Y, int64_t ldy, float* stats, void* stream);
 int launch_norm_backward(const NormProblem& p, int dtype, const NormGrads& g, float* ws, void* stream);
 
-// out[i] (+)= sum over parts, in ascending order within a fixed tree, of ws[part * stride + first + i].
-int launch_sum_parts(const float* ws, int64_t parts, int64_t stride, int64_t first, int64_t count, float* out, int accumulate,
+// out[i] (+)= sum over the parts, in a fixed order, of ws[part * stride + first + i], i < count (0: not wanted; one of them is).
+struct SumTarget {
+  float* out;
+  int64_t first, count;
+};
+int launch_sum_parts(const float* ws, int64_t parts, int64_t stride, const SumTarget& t0, const SumTarget& t1, int accumulate,
                      void* stream);
 
 // ---------------------------------------------------------------- linear layer (linear.hip)

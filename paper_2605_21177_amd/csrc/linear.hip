@@ -19,18 +19,37 @@ namespace chunkft {
 
 namespace {
 
+// The normal distribution's integral up to z and e^(-z^2 / 2).  erfc by Hastings' rational form (Abramowitz and Stegun 7.1.26, off
+// by at most 1.5e-7): a reciprocal, an exponential and six products where the library's erf is three times that, and the
+// epilogue of a 256 x 256 tile was 40 us of it (1024 x 4096 x 14336 with bias, GELU and z: 143 us).
+__device__ __forceinline__ float normal_cdf(float z, float& bell) {
+  bell = __builtin_amdgcn_exp2f(-0.72134752f * z * z);
+  const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f * 0.70710678f, fabsf(z), 1.f));
+  const float p = fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
+  const float tail = 0.5f * t * p * bell;
+  return z < 0.f ? tail : 1.f - tail;
+}
+
+// v_exp_f32 and v_rcp_f32 are good to one step of the result: three roundings of 2^-23 instead of one
+__device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.44269504f * z)); }
+
 __device__ __forceinline__ float activate(float z, int act) {
   if (act == ACT_RELU) return z > 0.f ? z : (z != z ? z : 0.f);
-  if (act == ACT_GELU) return z * 0.5f * (1.f + erff(z * 0.70710678f));
-  if (act == ACT_SILU) return z / (1.f + expf(-z));
+  float bell;
+  if (act == ACT_GELU) return z * normal_cdf(z, bell);
+  if (act == ACT_SILU) return z * sigmoid(z);
   return z;
 }
 
 __device__ __forceinline__ float slope(float z, int act) {
   if (act == ACT_RELU) return z > 0.f ? 1.f : 0.f;
-  if (act == ACT_GELU) return 0.5f * (1.f + erff(z * 0.70710678f)) + z * expf(-0.5f * z * z) * 0.39894228f;
-  const float s = 1.f / (1.f + expf(-z));
-  return s * (1.f + z * (1.f - s));
+  if (act == ACT_GELU) {
+    float bell;
+    const float cdf = normal_cdf(z, bell);
+    return fmaf(0.39894228f * z, bell, cdf);
+  }
+  const float s = sigmoid(z);
+  return s * fmaf(z, 1.f - s, 1.f);
 }
 
 // What a product's row piece becomes: N consecutive columns of row m.
@@ -286,7 +305,7 @@ int launch_gate(const LinearProblem& p, const LinearGrads& g, float* ws, hipStre
   if (g.db) hipLaunchKernelGGL((gate_kernel<T, true>), grid, threads, 0, st, (const T*)g.dY, g.lddy, (const T*)g.Z, g.ldz, (T*)g.dZ, g.lddz, p.T, p.out, p.act, ws, pitch);
   else hipLaunchKernelGGL((gate_kernel<T, false>), grid, threads, 0, st, (const T*)g.dY, g.lddy, (const T*)g.Z, g.ldz, (T*)g.dZ, g.lddz, p.T, p.out, p.act, ws, pitch);
   int err = (int)hipGetLastError();
-  if (err == 0 && g.db) err = launch_sum_parts(ws, parts, pitch, g.b0, g.b1 - g.b0, g.db, g.accumulate, st);
+  if (err == 0 && g.db) err = launch_sum_parts(ws, parts, pitch, SumTarget{g.db, g.b0, g.b1 - g.b0}, SumTarget{nullptr, 0, 0}, g.accumulate, st);
   return err;
 }
 

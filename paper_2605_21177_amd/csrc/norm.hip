@@ -153,13 +153,17 @@ __global__ __launch_bounds__(kWideThreads) void norm_forward_wide_kernel(const N
 }
 
 // --------------------------------------------------------------------------------------------------- backward
-// A workgroup of R rows at a time walks the tokens in steps of the grid and keeps the sums of dy xh and dy over its tokens in
-// registers; at the end its R groups meet in LDS, in order, and leave one partial row of each.
+// A workgroup of R rows at a time walks the tokens in steps of the grid (two workgroups a compute unit, one computing while the
+// other waits at its row's barrier) and keeps the sums of dy xh and dy over its tokens in registers; the next rows are requested
+// before the present ones are finished.  At the end its R groups meet in LDS, in order, and leave one partial row of each sum.
+// 8192 tokens x 4096, bf16: 82 us without the request ahead, one workgroup a unit, and conversions in integer arithmetic.
 template <int G> constexpr int kBackThreads = G > 512 ? G : 512;
 
 template <typename T, int SUB, int G, int PC, bool SUMS>
-__global__ __launch_bounds__(kBackThreads<G>) void norm_backward_kernel(const NormProblem p, const NormGrads g, float* ws, int64_t pitch) {
+__global__ __launch_bounds__(kBackThreads<G>, 4) void norm_backward_kernel(const NormProblem p, const NormGrads g, float* ws,
+                                                                                       int64_t pitch) {
   constexpr int NT = kBackThreads<G>, R = NT / G, VE = Row<T>::N;
+  constexpr bool AHEAD = PC <= 2;                 // the registers hold two rows
   __shared__ float red[2][R][2 * (G / 64)];
   __shared__ float meet[SUMS && R > 1 ? 2 * NT * VE : 1];
   const int sub = threadIdx.x / G, l = threadIdx.x % G;
@@ -170,55 +174,70 @@ __global__ __launch_bounds__(kBackThreads<G>) void norm_backward_kernel(const No
     for (int e = 0; e < VE; ++e) sw[i][e] = sb[i][e] = 0.f;
   const T* const X = (const T*)p.X;
   const T* const dY = (const T*)g.dY;
+  Row<T> w[PC], x[PC], d[PC];
+#pragma unroll
+  for (int i = 0; i < PC; ++i) {
+    const int64_t c = (int64_t)(i * G + l) * VE;
+    if (p.w) {
+      w[i].load((const T*)p.w + c, p.n - c);
+    } else {
+      float one[VE];
+#pragma unroll
+      for (int e = 0; e < VE; ++e) one[e] = 1.f;
+      w[i].from(one);
+    }
+  }
+  auto request = [&](int64_t row, Row<T> (&a)[PC], Row<T> (&b)[PC]) {
+#pragma unroll
+    for (int i = 0; i < PC; ++i) {
+      const int64_t c = (int64_t)(i * G + l) * VE;
+      a[i].load(X + row * p.ldx + c, p.n - c);
+      b[i].load(dY + row * g.lddy + c, p.n - c);
+    }
+  };
+  const float inv_n = 1.f / (float)p.n;
+  const int64_t step = (int64_t)gridDim.x * R;
   int buf = 0;
-  for (int64_t t0 = (int64_t)blockIdx.x * R; t0 < p.T; t0 += (int64_t)gridDim.x * R) {
-    const int64_t t = t0 + sub;
+  int64_t t = (int64_t)blockIdx.x * R + sub;
+  if constexpr (AHEAD) request(t < p.T ? t : p.T - 1, x, d);
+  for (int64_t t0 = (int64_t)blockIdx.x * R; t0 < p.T; t0 += step, t += step) {
     const bool here = t < p.T;
     const int64_t row = here ? t : p.T - 1;
-    Row<T> x[PC], d[PC];
-#pragma unroll
-    for (int i = 0; i < PC; ++i) {
-      const int64_t c = (int64_t)(i * G + l) * VE;
-      x[i].load(X + row * p.ldx + c, p.n - c);
-      d[i].load(dY + row * g.lddy + c, p.n - c);
-    }
+    if constexpr (!AHEAD) request(row, x, d);
     const float mean = SUB ? g.stats[2 * row] : 0.f, rstd = g.stats[2 * row + 1];
-    float s[2] = {0.f, 0.f};
+    // what lies behind the end of a row is zero in x, dy and w: h and the sums of dy take nothing from it, xh only meets dy = 0
+    float xh[PC][VE], h[PC][VE], s[2] = {0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < PC; ++i) {
-      const int64_t c = (int64_t)(i * G + l) * VE;
-      Row<T> w;
-      if (p.w && g.dX) w.load((const T*)p.w + c, p.n - c);
+    for (int i = 0; i < PC; ++i)
 #pragma unroll
       for (int e = 0; e < VE; ++e) {
-        if (c + e >= p.n) break;
-        const float xh = (x[i].at(e) - mean) * rstd, h = p.w ? d[i].at(e) * w.at(e) : d[i].at(e);
-        if constexpr (SUB) s[0] += h;
-        s[1] = fmaf(h, xh, s[1]);
+        const float dy = d[i].at(e);
+        xh[i][e] = (x[i].at(e) - mean) * rstd;
+        h[i][e] = dy * w[i].at(e);
+        if constexpr (SUB) s[0] += h[i][e];
+        s[1] = fmaf(h[i][e], xh[i][e], s[1]);
         if constexpr (SUMS) {
-          if (here) {
-            sw[i][e] = fmaf(d[i].at(e), xh, sw[i][e]);
-            sb[i][e] += d[i].at(e);
-          }
+          const float mine = R > 1 && !here ? 0.f : dy;
+          sw[i][e] = fmaf(mine, xh[i][e], sw[i][e]);
+          sb[i][e] += mine;
         }
       }
+    if constexpr (AHEAD) {
+      const int64_t next = t + step;
+      if (t0 + step < p.T) request(next < p.T ? next : p.T - 1, x, d);
     }
     if (g.dX) {
       row_sum<G>(s, red[buf][sub], l);
       buf ^= 1;
-      const float c1 = s[0] / (float)p.n, c2 = s[1] / (float)p.n;
+      const float c1 = s[0] * inv_n, c2 = s[1] * inv_n;
 #pragma unroll
       for (int i = 0; i < PC; ++i) {
         const int64_t c = (int64_t)(i * G + l) * VE;
         if (!here || c >= p.n) continue;
-        Row<T> w, o;
-        if (p.w) w.load((const T*)p.w + c, p.n - c);
         float f[VE];
 #pragma unroll
-        for (int e = 0; e < VE; ++e) {
-          const float xh = (x[i].at(e) - mean) * rstd, h = p.w ? d[i].at(e) * w.at(e) : d[i].at(e);
-          f[e] = (h - c1 - xh * c2) * rstd;
-        }
+        for (int e = 0; e < VE; ++e) f[e] = (SUB ? fmaf(-xh[i][e], c2, h[i][e] - c1) : fmaf(-xh[i][e], c2, h[i][e])) * rstd;
+        Row<T> o;
         o.from(f);
         o.store((T*)g.dX + t * g.lddx + c, p.n - c);
       }
@@ -238,12 +257,14 @@ __global__ __launch_bounds__(kBackThreads<G>) void norm_backward_kernel(const No
         }
         __syncthreads();
         if (sub == 0) {
+#pragma unroll 1
+          for (int k = 1; k < R; ++k) {
 #pragma unroll
-          for (int e = 0; e < VE; ++e)
-            for (int k = 1; k < R; ++k) {
+            for (int e = 0; e < VE; ++e) {
               sw[i][e] += meet[(k * VE + e) * G + l];
               sb[i][e] += meet[NT * VE + (k * VE + e) * G + l];
             }
+          }
         }
       }
       if (sub == 0) {
@@ -324,16 +345,18 @@ __global__ __launch_bounds__(kWideCols) void norm_wide_sums_kernel(const NormPro
   }
 }
 
-// 32 columns (a 128-byte line of a partial row) by 32 lanes along the parts, joined in LDS in order.
+// 32 columns (a 128-byte line of a partial row) by 32 lanes along the parts, joined in LDS in order.  One row of blocks per vector.
 constexpr int kSumCols = 32, kSumLanes = 32;
-__global__ __launch_bounds__(kSumCols * kSumLanes) void sum_parts_kernel(const float* ws, int64_t parts, int64_t stride, int64_t first,
-                                                                        int64_t count, float* out, int accumulate) {
+__global__ __launch_bounds__(kSumCols * kSumLanes) void sum_parts_kernel(const float* ws, int64_t parts, int64_t stride, const SumTarget t0,
+                                                                        const SumTarget t1, int accumulate) {
   __shared__ float red[kSumLanes][kSumCols + 1];
+  const SumTarget t = blockIdx.y == 0 ? t0 : t1;
+  if ((int64_t)blockIdx.x * kSumCols >= t.count) return;
   const int c = threadIdx.x % kSumCols, k = threadIdx.x / kSumCols;
   const int64_t i = (int64_t)blockIdx.x * kSumCols + c;
   float s = 0.f;
-  if (i < count)
-    for (int64_t q = k; q < parts; q += kSumLanes) s += ws[q * stride + first + i];
+  if (i < t.count)
+    for (int64_t q = k; q < parts; q += kSumLanes) s += ws[q * stride + t.first + i];
   red[k][c] = s;
   __syncthreads();
 #pragma unroll
@@ -341,28 +364,29 @@ __global__ __launch_bounds__(kSumCols * kSumLanes) void sum_parts_kernel(const f
     if (k < h) red[k][c] += red[k + h][c];
     __syncthreads();
   }
-  if (k == 0 && i < count) out[i] = accumulate ? out[i] + red[0][c] : red[0][c];
+  if (k == 0 && i < t.count) t.out[i] = accumulate ? t.out[i] + red[0][c] : red[0][c];
 }
 
 // lanes per row and pieces per lane for a row of n elements; 0 lanes: wide
 struct Shape { int lanes, pieces; };
 Shape shape_of(int64_t n, int dtype) {
   const int64_t pieces = ceil_div(n, dtype == 0 ? 4 : 8);
-  if (pieces <= 64) return {64, 1};
-  if (pieces <= 128) return {64, 2};
-  if (pieces <= 256) return {64, 4};
-  if (pieces <= 512) return {256, 2};
-  if (pieces <= 1024) return {256, 4};
-  if (pieces <= 2048) return {1024, 2};
+  for (int lanes = 64; lanes <= 1024; lanes *= 2)
+    if (pieces <= 2 * lanes) return {lanes, pieces <= lanes ? 1 : 2};
   if (pieces <= 4096) return {1024, 4};
   return {0, 0};
 }
 
 template <class F>
 int with_shape(const Shape& s, F&& f) {
-  if (s.lanes == 64) return s.pieces == 1 ? f(IntC<64>{}, IntC<1>{}) : s.pieces == 2 ? f(IntC<64>{}, IntC<2>{}) : f(IntC<64>{}, IntC<4>{});
-  if (s.lanes == 256) return s.pieces == 2 ? f(IntC<256>{}, IntC<2>{}) : f(IntC<256>{}, IntC<4>{});
-  return s.pieces == 2 ? f(IntC<1024>{}, IntC<2>{}) : f(IntC<1024>{}, IntC<4>{});
+  if (s.pieces == 4) return f(IntC<1024>{}, IntC<4>{});
+  switch (s.lanes) {
+    case 64: return s.pieces == 1 ? f(IntC<64>{}, IntC<1>{}) : f(IntC<64>{}, IntC<2>{});
+    case 128: return f(IntC<128>{}, IntC<2>{});
+    case 256: return f(IntC<256>{}, IntC<2>{});
+    case 512: return f(IntC<512>{}, IntC<2>{});
+    default: return f(IntC<1024>{}, IntC<2>{});
+  }
 }
 
 int rows_at_once(const Shape& s) { return s.lanes > 512 ? 1 : 512 / s.lanes; }
@@ -408,26 +432,29 @@ int backward_typed(const NormProblem& p, int dtype, const NormGrads& g, float* w
     });
   }
   int err = (int)hipGetLastError();
-  if (err == 0 && g.dw) err = launch_sum_parts(ws, parts, 2 * pitch, g.w0, g.w1 - g.w0, g.dw, g.accumulate, st);
-  if (err == 0 && g.db) err = launch_sum_parts(ws, parts, 2 * pitch, pitch + g.b0, g.b1 - g.b0, g.db, g.accumulate, st);
-  return err;
+  if (err != 0 || !sums) return err;
+  return launch_sum_parts(ws, parts, 2 * pitch, SumTarget{g.dw, g.w0, g.dw ? g.w1 - g.w0 : 0},
+                          SumTarget{g.db, pitch + g.b0, g.db ? g.b1 - g.b0 : 0}, g.accumulate, st);
 }
 
 }  // namespace
 
 int64_t norm_parts(int64_t T, int64_t n, int dtype, int compute_units) {
   const Shape s = shape_of(n, dtype);
-  const int64_t most = s.lanes ? compute_units : 64;
+  // two workgroups a compute unit (one of 1024 lanes)
+  const int64_t most = s.lanes ? (s.lanes > 512 ? 1 : 2) * (int64_t)compute_units : 64;
   const int64_t need = ceil_div(T, s.lanes ? rows_at_once(s) : 1);
   return need < most ? need : most;
 }
 
-int launch_sum_parts(const float* ws, int64_t parts, int64_t stride, int64_t first, int64_t count, float* out, int accumulate,
+int launch_sum_parts(const float* ws, int64_t parts, int64_t stride, const SumTarget& t0, const SumTarget& t1, int accumulate,
                      void* stream) {
-  const int64_t blocks = ceil_div(count, kSumCols);
-  if (blocks > kMaxLaunchThreads / (kSumCols * kSumLanes)) return (int)hipErrorInvalidValue;
-  hipLaunchKernelGGL(sum_parts_kernel, dim3((unsigned)blocks), dim3(kSumCols * kSumLanes), 0, (hipStream_t)stream, ws, parts, stride,
-                     first, count, out, accumulate);
+  const SumTarget& a = t0.count > 0 ? t0 : t1;
+  const SumTarget& b = t0.count > 0 ? t1 : t0;
+  const int64_t blocks = ceil_div(a.count > b.count ? a.count : b.count, kSumCols);
+  if (blocks > kMaxLaunchThreads / (kSumCols * kSumLanes) / 2) return (int)hipErrorInvalidValue;
+  hipLaunchKernelGGL(sum_parts_kernel, dim3((unsigned)blocks, b.count > 0 ? 2 : 1), dim3(kSumCols * kSumLanes), 0, (hipStream_t)stream, ws,
+                     parts, stride, a, b, accumulate);
   return (int)hipGetLastError();
 }
 

@@ -6,6 +6,8 @@
 
 namespace chunkft {
 
+typedef __attribute__((ext_vector_type(2))) float f32x2;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(8))) float f32x8;
 typedef unsigned int u32x4_a2 __attribute__((ext_vector_type(4), aligned(2)));   // 16 bytes at any bf16
@@ -64,11 +66,11 @@ template <> struct Row<unsigned short> {
   __device__ __forceinline__ float at(int i) const {
     return __uint_as_float(i & 1 ? v[i / 2] & 0xffff0000u : v[i / 2] << 16);
   }
-  // the one rounding of a result to its 16-bit type: to nearest, ties to even
+  // the one rounding of a result to its 16-bit type: to nearest, ties to even (v_cvt_pk_bf16_f32, two values an instruction)
   __device__ __forceinline__ void from(const float* f) {
 #pragma unroll
     for (int e = 0; e < N / 2; ++e)
-      v[e] = (unsigned)f32_to_bf16_rne(f[2 * e]) | ((unsigned)f32_to_bf16_rne(f[2 * e + 1]) << 16);
+      v[e] = __builtin_bit_cast(unsigned, __builtin_convertvector((f32x2{f[2 * e], f[2 * e + 1]}), bf16x2));
   }
 };
 
