@@ -84,7 +84,7 @@ int launch_linear_backward(const LinearProblem& p, const LinearGrads& g, float* 
 // ------------------------------------------------------- orthogonalised update (orthogonalize.hip)
 struct OrthoProblem {
   int64_t rows, cols;
-  int32_t planes;        // 1: 16-bit operands, 2: 22-bit operands
+  int32_t parts;         // of the products' operands: 1: 11 digits, 2: 22
   int32_t steps;
   float eps;
   // what is orthogonalised: G (bf16 or fp32), or the momentum step on g and m
@@ -104,7 +104,7 @@ struct OrthoProblem {
   float lr, scale, weight_decay;
 };
 
-size_t ortho_workspace_bytes(int64_t rows, int64_t cols, int planes);
+size_t ortho_workspace_bytes(int64_t rows, int64_t cols, int parts);
 int launch_orthogonalize(const OrthoProblem& p, void* ws, void* stream);
 
 }  // namespace chunkft

@@ -184,7 +184,7 @@ extern "C" int chunkft_orthogonalize(const void* G, int64_t ldg, int32_t dtype, 
   OrthoProblem p{};
   p.rows = rows;
   p.cols = cols;
-  p.planes = dtype == CHUNKFT_F32 ? 2 : 1;
+  p.parts = dtype == CHUNKFT_F32 ? 2 : 1;
   p.steps = steps;
   p.eps = static_cast<float>(eps);
   p.G = G;
@@ -193,7 +193,7 @@ extern "C" int chunkft_orthogonalize(const void* G, int64_t ldg, int32_t dtype, 
   p.O = O;
   p.ldo = ldo;
   p.o_dtype = dtype;
-  if (s == CHUNKFT_OK) s = check_workspace(ws, ws_bytes, ortho_workspace_bytes(rows, cols, p.planes), 256);
+  if (s == CHUNKFT_OK) s = check_workspace(ws, ws_bytes, ortho_workspace_bytes(rows, cols, p.parts), 256);
   if (s != CHUNKFT_OK) return s;
   return done(launch_orthogonalize(p, ws, stream));
 }
@@ -210,7 +210,7 @@ extern "C" int chunkft_muon_chunk(const float* g, float* master, float* m, void*
   OrthoProblem p{};
   p.rows = rows;
   p.cols = cols;
-  p.planes = hp->precision == CHUNKFT_F32 ? 2 : 1;
+  p.parts = hp->precision == CHUNKFT_F32 ? 2 : 1;
   p.steps = hp->steps;
   p.eps = static_cast<float>(hp->eps);
   p.G = g;
@@ -225,7 +225,7 @@ extern "C" int chunkft_muon_chunk(const float* g, float* master, float* m, void*
   p.lr = static_cast<float>(hp->lr);
   p.scale = static_cast<float>(hp->scale);
   p.weight_decay = static_cast<float>(hp->weight_decay);
-  const int s = check_workspace(ws, ws_bytes, ortho_workspace_bytes(rows, cols, p.planes), 256);
+  const int s = check_workspace(ws, ws_bytes, ortho_workspace_bytes(rows, cols, p.parts), 256);
   if (s != CHUNKFT_OK) return s;
   return done(launch_orthogonalize(p, ws, stream));
 }

@@ -106,7 +106,7 @@ __device__ __forceinline__ P slab_of(P q, const Slabs& s, int slab) {
 }
 
 template <class C, int KB, bool DMA, bool SPLIT>
-__global__ __launch_bounds__(C::NT, C::MINW) void linear_kernel(const Product whole, const TileOrder o, int n_items, const Epilogue e,
+__global__ __launch_bounds__(C::NT, 2) void linear_kernel(const Product whole, const TileOrder o, int n_items, const Epilogue e,
                                                                 const Slabs s) {
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
   const int item = xcd_work_item(n_items);
@@ -318,8 +318,8 @@ bool fill_order(int64_t M, int64_t N, int64_t bm, int64_t bn, int threads, int s
   return true;
 }
 
-typedef ProductCfg<256, 256, 64, 4, 2, 3, 2> Tile256;
-typedef ProductCfg<128, 128, 64, 2, 2, 2, 2> Tile128;
+typedef ProductCfg<256, 256, 4, 2, 3, 2> Tile256;
+typedef ProductCfg<128, 128, 2, 2, 2, 2> Tile128;
 
 template <class C, int KB, bool DMA, bool SPLIT>
 int launch_tiles(const Product& q, const Epilogue& e, const Slabs& s, hipStream_t st) {
@@ -360,7 +360,7 @@ int launch_product(const void* A, int64_t lda, const void* B, int64_t ldb, int64
     else err = plan.tile == 128 ? launch_tiles_f32<128, 128, KB, false>(q, e, s, st) : launch_tiles_f32<64, 64, KB, false>(q, e, s, st);
     return err != 0 || plan.slabs == 1 ? err : join_slabs<float>(s, M, N, e, st);
   }
-  const Product q{(const unsigned short*)A, (const unsigned short*)B, lda, ldb, 0, 0, M, N, K};
+  const Product q{(const unsigned short*)A, (const unsigned short*)B, lda, ldb, M, N, K};
   const bool direct = direct_rows(A, lda, K, false) && direct_rows(B, ldb, N, KB != 0);
   if (plan.slabs > 1) {
     if (!direct) err = launch_tiles<Tile128, KB, false, true>(q, e, s, st);

@@ -6,35 +6,25 @@
 // near one.  The products of the small side r = min(rows, cols): where rows > cols the matrix stays as it lies and A = X^T X,
 // X <- X (a I + b A + c A^2).  A and its polynomial are symmetric: half of their tiles are computed and stored twice.
 //
-// The products run on the fp16 matrix instruction, from one plane (11-bit operands, for results of 8 bits) or two (x = hi + lo,
-// 22 bits, for fp32 results: hi hi + hi lo + lo hi, three instructions for one).  fp16 because every quantity has a known
+// The products run on the fp16 matrix instruction, on operands of one part (11 digits, for results of 8) or two (x = hi + lo, 22
+// digits, for fp32 results: hi hi + hi lo + lo hi, three instructions for one).  fp16 because every quantity has a known
 // bound: singular values stay below 1.21, so entries of X are held times 2^14, of A times 2^14, of the polynomial (at most
 // 3.45) times 2^13.  U itself is held times a power of two that brings its norm to 2^14 .. 2^15, exactly where U is bf16, and
 // 1 / (|U| + eps) is applied in fp32 to the first step's sums: a rounding of X before the first step would be amplified by a^5.
-// The planes are padded with zeros to whole tiles, which the steps keep: no product has an edge.
+// The matrices are padded with zeros to multiples of 64, whole stages of the products' k, and the steps keep the zeros.
 #include <hip/hip_runtime.h>
 
-#include "internal.h"
-#include "launch.h"
-#include "layers.h"
-#include "pieces.h"
-#include "product.h"
+#include <cmath>
+
+#include "newton_schulz_steps.h"
 
 namespace chunkft {
 
 namespace {
 
-constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
-constexpr float kScaleX = 16384.f, kScaleA = 16384.f, kScaleP = 8192.f;
 constexpr int kNormBlocks = 1024;                // most partial sums of the norm
-constexpr int64_t kPad = 128;                    // planes are whole tiles
 
-struct Scalars {
-  float up;      // planes of U hold U * up
-  float down;    // X = plane * down, before the first step
-};
-
-// ------------------------------------------------------------------------------ momentum, norm, planes
+// ------------------------------------------------------------------------------ momentum, norm, parts
 // G as `lines` lines of `len` elements: a matrix without padding is one line.
 struct Source {
   const void* G;
@@ -81,7 +71,7 @@ __global__ __launch_bounds__(256) void momentum_norm_kernel(const Source s, doub
   if (threadIdx.x == 0) parts[blockIdx.y * gridDim.x + blockIdx.x] = red[0] + red[1] + red[2] + red[3];
 }
 
-__global__ __launch_bounds__(256) void scalars_kernel(const double* parts, int n, float eps, Scalars* out) {
+__global__ __launch_bounds__(256) void scalars_kernel(const double* parts, int n, float eps, NsScalars* out) {
   __shared__ double red[256];
   double sum = 0.0;
   for (int i = threadIdx.x; i < n; i += 256) sum += parts[i];
@@ -93,7 +83,7 @@ __global__ __launch_bounds__(256) void scalars_kernel(const double* parts, int n
   }
   if (threadIdx.x != 0) return;
   const double norm = sqrt(red[0]);
-  Scalars r{1.f, 0.f};
+  NsScalars r{1.f, 0.f};
   if (!(norm < 1.7e308)) {
     r.down = __uint_as_float(0x7fc00000u);       // a norm that is no number makes every result none
   } else if (norm > 0.0) {
@@ -107,35 +97,9 @@ __global__ __launch_bounds__(256) void scalars_kernel(const double* parts, int n
   *out = r;
 }
 
-typedef __attribute__((ext_vector_type(8))) _Float16 h8;
-
-// x as one or two planes at p.
-template <int NP>
-__device__ __forceinline__ void store_planes(unsigned short* p, int64_t plane, const float (&x)[8]) {
-  h8 hi, lo;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    hi[e] = (_Float16)x[e];
-    if constexpr (NP == 2) lo[e] = (_Float16)(x[e] - (float)hi[e]);
-  }
-  *(h8*)p = hi;
-  if constexpr (NP == 2) *(h8*)(p + plane) = lo;
-}
-template <int NP>
-__device__ __forceinline__ void load_planes(const unsigned short* p, int64_t plane, float (&x)[8]) {
-  const h8 hi = *(const h8*)p;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) x[e] = (float)hi[e];
-  if constexpr (NP == 2) {
-    const h8 lo = *(const h8*)(p + plane);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] += (float)lo[e];
-  }
-}
-
 template <typename T, int NP>
-__global__ __launch_bounds__(256) void planes_kernel(const T* G, int64_t ldg, const float* m, float momentum, bool nesterov, int64_t rows,
-                                                     int64_t cols, int64_t rows_p, int64_t cols_p, const Scalars* sc,
+__global__ __launch_bounds__(256) void hold_kernel(const T* G, int64_t ldg, const float* m, float momentum, bool nesterov, int64_t rows,
+                                                     int64_t cols, int64_t rows_p, int64_t cols_p, const NsScalars* sc,
                                                      unsigned short* X) {
   const float up = sc->up;
   const int64_t per_row = cols_p / 8, n = rows_p * per_row;
@@ -162,184 +126,36 @@ __global__ __launch_bounds__(256) void planes_kernel(const T* G, int64_t ldg, co
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] *= up;
-    store_planes<NP>(X + r * cols_p + c, rows_p * cols_p, x);
+    store_parts<NP>(X + r * cols_p * NP + stored<NP>(c), x);
   }
 }
 
-// ------------------------------------------------------------------------------------- products of a step
-enum Step : int { GRAM = 0, POLY = 1, APPLY = 2, LAST = 3 };
-
-struct StepArgs {
-  Product q;
-  TileOrder order;               // APPLY, LAST
-  int n_items;
-  const Scalars* sc;             // nullptr after the first step
-  unsigned short* D;             // planes that the step writes
-  int64_t ldd, plane_d;
-  // LAST
-  int64_t rows, cols, ldo;
-  void* O;
-  int32_t o_dtype, w_kind;
-  float* master;
-  void* W;
-  float lr, scale, weight_decay;
-};
-
-__device__ __forceinline__ void tile_of_half(int item, int& i, int& j) {
-  int r = (int)((sqrtf(8.f * (float)item + 1.f) - 1.f) * 0.5f);
-  while (r * (r + 1) / 2 > item) --r;
-  while ((r + 1) * (r + 2) / 2 <= item) ++r;
-  i = r;
-  j = item - r * (r + 1) / 2;
-}
-
-template <typename T>
-__device__ __forceinline__ void put_result(T* p, int64_t valid, const float (&v)[8]) {
-#pragma unroll
-  for (int h = 0; h < 8; h += Row<T>::N) {
-    Row<T> x;
-    x.from(v + h);
-    x.store(p + h, valid - h);
-  }
-}
-
-template <class C, int STEP, int KA, int KB>
-__global__ __launch_bounds__(C::NT, C::MINW) void step_kernel(const StepArgs s) {
-  extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
-  constexpr bool HALF = STEP == GRAM || STEP == POLY;
-  static_assert(!HALF || C::BM == C::BN, "tiles of a symmetric result");
-  const int item = xcd_work_item(s.n_items);
-  if (item < 0) return;
-  int tm, tn;
-  if constexpr (HALF) tile_of_half(item, tm, tn);
-  else tile_at(s.order, item, tm, tn);
-  const int64_t row0 = (int64_t)tm * C::BM, col0 = (int64_t)tn * C::BN;
-  const float down = s.sc ? s.sc->down : 1.f / kScaleX;
-  const float f = STEP == GRAM ? down * down : STEP == POLY ? 1.f / (kScaleA * kScaleA) : down / kScaleP;
-  product_tile<C, KA, KB, true, true>(s.q, row0, col0, lds, [&](int m, int n, float (&v)[8]) {
-    const int64_t r = row0 + m, c = col0 + n;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] *= f;
-    if constexpr (STEP == LAST) {
-      if (r >= s.rows || c >= s.cols) return;
-      const int64_t valid = s.cols - c;
-      if (!s.master) {
-        if (s.o_dtype == 0) put_result((float*)s.O + r * s.ldo + c, valid, v);
-        else put_result((unsigned short*)s.O + r * s.ldo + c, valid, v);
-        return;
-      }
-      const int64_t at = r * s.cols + c;
-#pragma unroll
-      for (int h = 0; h < 8; h += 4) {
-        Row<float> th;
-        th.load(s.master + at + h, valid - h);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[h + e] = fmaf(-s.lr, fmaf(s.scale, v[h + e], s.weight_decay * th.v[e]), th.v[e]);
-      }
-      put_result(s.master + at, valid, v);
-      if (s.w_kind == W_BF16) put_result((unsigned short*)s.W + at, valid, v);
-      else if (s.w_kind == W_F32) put_result((float*)s.W + at, valid, v);
-    } else {
-      if constexpr (STEP == POLY) {
-        float a[8];
-        load_planes<C::NP>(s.q.A + r * s.q.lda + c, s.q.plane_a, a);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = fmaf(kC, v[e], kB * (a[e] * (1.f / kScaleA))) + (r == c + e ? kA : 0.f);
-      }
-      const float held = STEP == GRAM ? kScaleA : STEP == POLY ? kScaleP : kScaleX;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] *= held;
-      store_planes<C::NP>(s.D + r * s.ldd + c, s.plane_d, v);
-      if constexpr (HALF) {
-        if (tm != tn) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            unsigned short* const p = s.D + (c + e) * s.ldd + r;
-            const _Float16 hi = (_Float16)v[e];
-            *(_Float16*)p = hi;
-            if constexpr (C::NP == 2) *(_Float16*)(p + s.plane_d) = (_Float16)(v[e] - (float)hi);
-          }
-        }
-      }
-    }
-  });
-}
-
-template <class C, int STEP, int KA, int KB>
-int launch_step(StepArgs& s, hipStream_t st) {
-  const int64_t tm = ceil_div(s.q.M, C::BM), tn = ceil_div(s.q.N, C::BN);
-  const int64_t n = STEP == GRAM || STEP == POLY ? tm * (tm + 1) / 2 : tm * tn;
-  if (tm > 0x7fff || tn > 0x7fffff || n > kMaxLaunchThreads / C::NT - 8) return (int)hipErrorInvalidValue;
-  s.order = TileOrder{(int)tm, (int)tn, 8};
-  s.n_items = (int)n;
-  const int err = raise_lds_limit<step_kernel<C, STEP, KA, KB>>(C::LDS);
-  if (err != 0) return err;
-  hipLaunchKernelGGL((step_kernel<C, STEP, KA, KB>), dim3((unsigned)((n + 7) / 8 * 8)), dim3(C::NT), C::LDS, st, s);
-  return (int)hipGetLastError();
-}
-
-int64_t padded(int64_t n) { return (n + kPad - 1) / kPad * kPad; }
+int64_t padded(int64_t n) { return (n + kNsPad - 1) / kNsPad * kNsPad; }
 
 struct Layout {
   int64_t rows_p, cols_p, r;        // r: padded small side
-  size_t x, a, total;               // bytes of a buffer of X's planes, of A's, of all
+  size_t x, a, sums, total;         // bytes of a buffer of X, of A, of the slabs' sums, of all
 };
-Layout layout_of(int64_t rows, int64_t cols, int planes) {
+Layout layout_of(int64_t rows, int64_t cols, int parts) {
   Layout l;
   l.rows_p = padded(rows);
   l.cols_p = padded(cols);
   l.r = l.rows_p < l.cols_p ? l.rows_p : l.cols_p;
-  l.x = (size_t)l.rows_p * (size_t)l.cols_p * 2u * (size_t)planes;
-  l.a = (size_t)l.r * (size_t)l.r * 2u * (size_t)planes;
-  l.total = 256 + kNormBlocks * sizeof(double) + 2 * l.x + 2 * l.a;
+  const int64_t c = l.rows_p < l.cols_p ? l.cols_p : l.rows_p;
+  l.x = (size_t)l.rows_p * (size_t)l.cols_p * 2u * (size_t)parts;
+  l.a = (size_t)l.r * (size_t)l.r * 2u * (size_t)parts;
+  l.sums = 0;
+  for (int64_t k : {c, l.r}) {
+    const NsCut cut = ns_cut(l.r, k, parts, device_compute_units());
+    const size_t need = cut.slabs > 1 ? (size_t)cut.slabs * (size_t)ns_half_tiles(l.r, cut.tile) * (size_t)(cut.tile * cut.tile) * 4u : 0;
+    if (need > l.sums) l.sums = need;
+  }
+  l.total = 256 + kNormBlocks * sizeof(double) + 2 * l.x + 2 * l.a + l.sums;
   return l;
 }
 
-template <class C>
-int run_steps(const OrthoProblem& p, const Layout& l, const Scalars* sc, unsigned short* x0, unsigned short* x1, unsigned short* a,
-              unsigned short* poly, hipStream_t st) {
-  const bool tall = p.rows > p.cols;
-  const int64_t plane_x = l.rows_p * l.cols_p, plane_a = l.r * l.r;
-  int err = 0;
-  for (int k = 0; k < p.steps && err == 0; ++k) {
-    StepArgs s{};
-    s.sc = k == 0 ? sc : nullptr;
-    s.D = a;
-    s.ldd = l.r;
-    s.plane_d = plane_a;
-    s.q = Product{x0, x0, l.cols_p, l.cols_p, plane_x, plane_x, l.r, l.r, tall ? l.rows_p : l.cols_p};
-    err = tall ? launch_step<C, GRAM, 1, 1>(s, st) : launch_step<C, GRAM, 0, 0>(s, st);
-    if (err != 0) break;
-    s.D = poly;
-    s.q = Product{a, a, l.r, l.r, plane_a, plane_a, l.r, l.r, l.r};
-    err = launch_step<C, POLY, 0, 0>(s, st);
-    if (err != 0) break;
-    s.D = x1;
-    s.ldd = l.cols_p;
-    s.plane_d = plane_x;
-    s.q = tall ? Product{x0, poly, l.cols_p, l.r, plane_x, plane_a, l.rows_p, l.cols_p, l.r}
-               : Product{poly, x0, l.r, l.cols_p, plane_a, plane_x, l.rows_p, l.cols_p, l.r};
-    if (k + 1 < p.steps) {
-      err = tall ? launch_step<C, APPLY, 0, 0>(s, st) : launch_step<C, APPLY, 0, 1>(s, st);
-    } else {
-      s.rows = p.rows; s.cols = p.cols; s.ldo = p.ldo;
-      s.O = p.O; s.o_dtype = p.o_dtype;
-      s.master = p.master; s.W = p.W; s.w_kind = p.w_kind;
-      s.lr = p.lr; s.scale = p.scale; s.weight_decay = p.weight_decay;
-      err = tall ? launch_step<C, LAST, 0, 0>(s, st) : launch_step<C, LAST, 0, 1>(s, st);
-    }
-    unsigned short* const t = x0;
-    x0 = x1;
-    x1 = t;
-  }
-  return err;
-}
-
-typedef ProductCfg<128, 128, 64, 2, 2, 2, 2, 1> OnePlane;
-typedef ProductCfg<128, 128, 32, 2, 2, 2, 2, 2> TwoPlanes;
-
 template <typename T>
-int prepare_planes(const OrthoProblem& p, const Layout& l, double* parts, Scalars* sc, unsigned short* x, hipStream_t st) {
+int prepare(const OrthoProblem& p, const Layout& l, double* parts, NsScalars* sc, unsigned short* x, hipStream_t st) {
   Source s{p.G, p.ldg, p.rows, p.cols, p.m, p.momentum, p.nesterov};
   if (p.ldg == p.cols) s.lines = 1, s.len = p.rows * p.cols;
   const int64_t across = ceil_div(s.len, 256 * Row<T>::N);
@@ -350,31 +166,85 @@ int prepare_planes(const OrthoProblem& p, const Layout& l, double* parts, Scalar
   hipLaunchKernelGGL(scalars_kernel, dim3(1), dim3(256), 0, st, parts, gx * gy, p.eps, sc);
   const int64_t blocks = ceil_div(l.rows_p * (l.cols_p / 8), 256);
   const dim3 grid((unsigned)(blocks < 16384 ? blocks : 16384));
-  if (p.planes == 1)
-    hipLaunchKernelGGL((planes_kernel<T, 1>), grid, dim3(256), 0, st, (const T*)p.G, p.ldg, p.m, p.momentum, p.nesterov, p.rows, p.cols, l.rows_p, l.cols_p, sc, x);
+  if (p.parts == 1)
+    hipLaunchKernelGGL((hold_kernel<T, 1>), grid, dim3(256), 0, st, (const T*)p.G, p.ldg, p.m, p.momentum, p.nesterov, p.rows, p.cols, l.rows_p, l.cols_p, sc, x);
   else
-    hipLaunchKernelGGL((planes_kernel<T, 2>), grid, dim3(256), 0, st, (const T*)p.G, p.ldg, p.m, p.momentum, p.nesterov, p.rows, p.cols, l.rows_p, l.cols_p, sc, x);
+    hipLaunchKernelGGL((hold_kernel<T, 2>), grid, dim3(256), 0, st, (const T*)p.G, p.ldg, p.m, p.momentum, p.nesterov, p.rows, p.cols, l.rows_p, l.cols_p, sc, x);
   return (int)hipGetLastError();
 }
 
 }  // namespace
 
-size_t ortho_workspace_bytes(int64_t rows, int64_t cols, int planes) { return layout_of(rows, cols, planes).total; }
+extern template int run_newton_schulz<2>(const OrthoProblem& p, const NsBuffers& b, hipStream_t st);   // orthogonalize_two.hip
+
+// Time in us of `n` workgroups of a tile with ks values of k each.  Measured per 1024 k, one part / two: 128-wide tiles 10.2 / 19.5
+// alone on a compute unit and 14.5 / 38 the pair; 192-wide ones 12.5 / 31 where few units have one and 19.5 / 46 where all have;
+// 256-wide ones 18.5 / 51 and 26 / 70.  E.g. A for r = K = 4096, two parts: 228 us in 128-wide tiles (528 of them, two rounds), 186
+// in 192-wide (253, one round), 232 in 256-wide (136 on 256 units); r = 1024, K = 4096: 79 in one slab, 29 in four.
+double ns_rounds(int tile, int parts, double n, double ks, double units) {
+  const double k = ks / 1024;
+  if (tile == 128) {
+    const double pair = parts == 1 ? 14.5 : 38, alone = parts == 1 ? 10.2 : 19.5;
+    const double full = std::floor(n / (2 * units)), rest = n - full * 2 * units;
+    return full * (pair * k + 1) + (rest > units ? pair * k + 1 : rest > 0 ? alone * k + 1 : 0);
+  }
+  const double few = tile == 256 ? (parts == 1 ? 18.5 : 51) : (parts == 1 ? 12.5 : 31);
+  const double all = tile == 256 ? (parts == 1 ? 26 : 70) : (parts == 1 ? 19.5 : 46);
+  const double full = std::floor(n / units), rest = n / units - full;
+  return full * (all * k + 2) + (rest > 0 ? (few + (all - few) * rest) * k + 2 : 0);
+}
+
+// Slabs only in 128-wide tiles: where they pay there are few tiles.  Joining them costs a launch and their traffic at 4.5 TB/s.
+NsCut ns_cut(int64_t r, int64_t K, int parts, int compute_units) {
+  NsCut best{128, 1, K};
+  double least = -1;
+  for (int tile : {128, 192, 256}) {
+    const double tiles = (double)ns_half_tiles(r, tile);
+    for (int slabs = 1; slabs <= (tile == 128 ? 16 : 1); ++slabs) {
+      const int64_t ks = padded(ceil_div(K, slabs));
+      if (ceil_div(K, ks) != slabs || (slabs > 1 && ks < 128)) continue;
+      double cost = ns_rounds(tile, parts, tiles * slabs, (double)ks, compute_units);
+      if (slabs > 1) cost += 3 + tiles * (slabs + 1) * 65536 / 4.5e6;
+      if (least < 0 || cost < least) {
+        least = cost;
+        best = NsCut{tile, slabs, slabs > 1 ? ks : K};
+      }
+    }
+  }
+  return best;
+}
+
+int ns_apply_tile(int64_t rows, int64_t cols, int64_t K, int parts, int compute_units) {
+  auto cost = [&](int tile) {
+    return ns_rounds(tile, parts, (double)(ceil_div(rows, tile) * ceil_div(cols, tile)), (double)K, compute_units);
+  };
+  return cost(256) < cost(128) ? 256 : 128;
+}
+
+size_t ortho_workspace_bytes(int64_t rows, int64_t cols, int parts) { return layout_of(rows, cols, parts).total; }
 
 int launch_orthogonalize(const OrthoProblem& p, void* ws, void* stream) {
   hipStream_t st = (hipStream_t)stream;
-  const Layout l = layout_of(p.rows, p.cols, p.planes);
-  unsigned char* const base = (unsigned char*)ws;
-  Scalars* const sc = (Scalars*)base;
-  double* const parts = (double*)(base + 256);
-  unsigned char* const x = base + 256 + kNormBlocks * sizeof(double);
-  unsigned short* const x0 = (unsigned short*)x;
-  unsigned short* const x1 = (unsigned short*)(x + l.x);
-  unsigned short* const a = (unsigned short*)(x + 2 * l.x);
-  unsigned short* const poly = (unsigned short*)(x + 2 * l.x + l.a);
-  const int err = p.g_dtype == 0 ? prepare_planes<float>(p, l, parts, sc, x0, st) : prepare_planes<unsigned short>(p, l, parts, sc, x0, st);
+  const Layout l = layout_of(p.rows, p.cols, p.parts);
+  unsigned char* at = (unsigned char*)ws;
+  auto take = [&](size_t bytes) {
+    unsigned char* const q = at;
+    at += bytes;
+    return q;
+  };
+  NsScalars* const sc = (NsScalars*)take(256);
+  double* const parts = (double*)take(kNormBlocks * sizeof(double));
+  NsBuffers b{l.rows_p, l.cols_p, l.r, sc};
+  b.x0 = (unsigned short*)take(l.x);
+  b.x1 = (unsigned short*)take(l.x);
+  b.a = (unsigned short*)take(l.a);
+  b.poly = (unsigned short*)take(l.a);
+  b.sums = (float*)take(l.sums);
+  const int err = p.g_dtype == 0 ? prepare<float>(p, l, parts, sc, b.x0, st) : prepare<unsigned short>(p, l, parts, sc, b.x0, st);
   if (err != 0) return err;
-  return p.planes == 1 ? run_steps<OnePlane>(p, l, sc, x0, x1, a, poly, st) : run_steps<TwoPlanes>(p, l, sc, x0, x1, a, poly, st);
+  return p.parts == 1 ? run_newton_schulz<1>(p, b, st) : run_newton_schulz<2>(p, b, st);
 }
+
+template int run_newton_schulz<1>(const OrthoProblem& p, const NsBuffers& b, hipStream_t st);
 
 }  // namespace chunkft

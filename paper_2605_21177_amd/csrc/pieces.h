@@ -19,6 +19,7 @@ template <typename T> struct Row;
 template <> struct Row<float> {
   static constexpr int N = 4;
   f32x4 v;
+  __device__ __forceinline__ void zero() { v = f32x4{0.f, 0.f, 0.f, 0.f}; }
   __device__ __forceinline__ void load(const float* p, int64_t valid) {
     if (valid >= N) {
       v = *(const f32x4_u*)p;
@@ -46,6 +47,7 @@ template <> struct Row<float> {
 template <> struct Row<unsigned short> {
   static constexpr int N = 8;
   u32x4_t v;
+  __device__ __forceinline__ void zero() { v = u32x4_t{0, 0, 0, 0}; }
   __device__ __forceinline__ void load(const unsigned short* p, int64_t valid) {
     if (valid >= N) {
       v = *(const u32x4_a2*)p;
