@@ -21,7 +21,7 @@ LIB = os.path.join(PKG, "libchunkft.so")
 LIB_TIMELINE = os.path.join(PKG, "libchunkft_timeline.so")   # diagnostic twin: workgroups note their phase times
 
 SOURCES = ["kernels.hip", "wgrad_f32.hip", "wgrad_ragged.hip", "wgrad_small.hip", "static_ws.hip", "calib.hip", "norm.hip", "linear.hip",
-           "orthogonalize.hip", "orthogonalize_two.hip", "api.cpp", "layers_api.cpp", "shape.cpp", "plan.cpp", "mover.cpp"]
+           "orthogonalize.hip", "orthogonalize_two.hip", "api.cpp", "layers_api.cpp", "layers_shape.cpp", "shape.cpp", "plan.cpp", "mover.cpp"]
 
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

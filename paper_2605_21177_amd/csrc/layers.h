@@ -28,6 +28,14 @@ struct NormGrads {
   int accumulate;
 };
 
+// Lanes that hold a row and 16-byte pieces each of them has; 0 lanes: a row that a workgroup cannot hold.
+struct RowShape {
+  int32_t lanes, pieces;
+};
+RowShape norm_forward_shape(int64_t n, int dtype);
+RowShape norm_backward_shape(int64_t n, int dtype);
+constexpr int kNormBackThreads = 512;    // of a workgroup of the backward pass, if a row takes no more
+
 // Workgroups that a backward pass leaves partial sums of the vectors' gradients from; each leaves two rows of norm_pitch floats.
 int64_t norm_parts(int64_t T, int64_t n, int dtype, int compute_units);
 inline int64_t norm_pitch(int64_t n) { return (n + 31) / 32 * 32; }
@@ -65,6 +73,8 @@ struct LinearGrads {
   int64_t b0, b1;
   int accumulate;
 };
+
+constexpr int kGateLanes = 32, kGateRows = 8;       // of the pass over dy and z: lanes along the columns, rows at a time
 
 // Rows of partial sums (of norm_pitch(out) floats) that a backward pass leaves for the bias.
 int64_t linear_parts(int64_t T, int64_t out, int dtype, int compute_units);
@@ -104,7 +114,25 @@ struct OrthoProblem {
   float lr, scale, weight_decay;
 };
 
-size_t ortho_workspace_bytes(int64_t rows, int64_t cols, int parts);
+// How the product of an r x r result over K is cut: tiles of its lower half, slabs of kslab values of k.
+struct NsCut {
+  int32_t tile, slabs;
+  int64_t kslab;
+};
+NsCut ns_cut(int64_t r, int64_t K, int parts, int compute_units);
+int ns_apply_tile(int64_t rows, int64_t cols, int64_t K, int parts, int compute_units);
+inline int64_t ns_half_tiles(int64_t r, int tile) {
+  const int64_t n = (r + tile - 1) / tile;
+  return n * (n + 1) / 2;
+}
+
+constexpr int kNsNormBlocks = 1024;      // most partial sums of the norm
+struct NsLayout {
+  int64_t rows_p, cols_p, r;             // padded to whole stages of k; the padded small side
+  size_t x, a, sums, total;              // bytes of a buffer of X, of A, of the slabs' sums, of all
+};
+NsLayout ns_layout(int64_t rows, int64_t cols, int parts, int compute_units);
+
 int launch_orthogonalize(const OrthoProblem& p, void* ws, void* stream);
 
 }  // namespace chunkft

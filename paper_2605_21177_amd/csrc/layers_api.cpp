@@ -170,7 +170,7 @@ extern "C" int chunkft_linear_backward(const chunkft_linear* L, const void* dY, 
 
 extern "C" size_t chunkft_orthogonalize_workspace_bytes(int32_t precision, int64_t rows, int64_t cols) {
   if (!known_dtype(precision) || !matrix_ok(rows, cols)) return 0;
-  return ortho_workspace_bytes(rows, cols, precision == CHUNKFT_F32 ? 2 : 1);
+  return ns_layout(rows, cols, precision == CHUNKFT_F32 ? 2 : 1, device_compute_units()).total;
 }
 
 extern "C" int chunkft_orthogonalize(const void* G, int64_t ldg, int32_t dtype, int64_t rows, int64_t cols, int32_t steps, double eps,
@@ -193,7 +193,7 @@ extern "C" int chunkft_orthogonalize(const void* G, int64_t ldg, int32_t dtype, 
   p.O = O;
   p.ldo = ldo;
   p.o_dtype = dtype;
-  if (s == CHUNKFT_OK) s = check_workspace(ws, ws_bytes, ortho_workspace_bytes(rows, cols, p.parts), 256);
+  if (s == CHUNKFT_OK) s = check_workspace(ws, ws_bytes, ns_layout(rows, cols, p.parts, device_compute_units()).total, 256);
   if (s != CHUNKFT_OK) return s;
   return done(launch_orthogonalize(p, ws, stream));
 }
@@ -225,7 +225,7 @@ extern "C" int chunkft_muon_chunk(const float* g, float* master, float* m, void*
   p.lr = static_cast<float>(hp->lr);
   p.scale = static_cast<float>(hp->scale);
   p.weight_decay = static_cast<float>(hp->weight_decay);
-  const int s = check_workspace(ws, ws_bytes, ortho_workspace_bytes(rows, cols, p.parts), 256);
+  const int s = check_workspace(ws, ws_bytes, ns_layout(rows, cols, p.parts, device_compute_units()).total, 256);
   if (s != CHUNKFT_OK) return s;
   return done(launch_orthogonalize(p, ws, stream));
 }

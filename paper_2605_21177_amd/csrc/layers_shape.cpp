@@ -1,0 +1,164 @@
+// Host-side shape logic of the layers and of the orthogonalised updates: how work is cut, and the workspaces that follow from it.
+// Pure functions of the shapes and of the number of compute units.
+#include <cmath>
+#include <initializer_list>
+
+#include "layers.h"
+
+namespace chunkft {
+
+namespace {
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// What a cut costs, in us, from rounds of workgroups (n items of a tile with ks values of k each on so many compute units) and the
+// slabs' traffic.  Measured per 1024 k (and 1 - 2 us around them): bf16, 256-wide tiles, one to a unit, 19.5 where few units have
+// one and 24 where all have; 128-wide ones 10.2 alone on a unit, 14.5 the pair.  fp32: 22 and 18.2 for 64-wide ones alone and
+// each of several, 72 and 64.5 for 128-wide ones.  Slabs: 8 bytes per slab and element at 7 TB/s, and a launch.
+// E.g. bf16, 4096 x 4096 x 14336: 256-wide tiles 388 us, 128-wide 419; 512 x 14336 x 4096 one slab of 128-wide tiles 146, four 64;
+// 1024 x 14336 x 4096 162 and, four slabs of 256-wide tiles, 108.
+double round_cost(int dtype, int tile, double items, double ks, double units) {
+  const double k = ks / 1024;
+  if (dtype == 0) {
+    const double each = std::ceil(items / units);
+    return tile == 64 ? (each <= 1 ? 22 : 18.2 * each) * k : (each <= 1 ? 72 : 64.5 * each) * k;
+  }
+  if (tile == 256) {
+    const double full = std::floor(items / units), rest = items / units - full;
+    return full * (24 * k + 2) + (rest > 0 ? (19.5 + 4.5 * rest) * k + 2 : 0);
+  }
+  const double full = std::floor(items / (2 * units)), rest = items - full * 2 * units;
+  return full * (14.5 * k + 1) + (rest > units ? 14.5 * k + 1 : rest > 0 ? 10.2 * k + 1 : 0);
+}
+
+// Time in us of `n` workgroups of a tile with ks values of k each.  Measured per 1024 k, one part / two: 128-wide tiles 10.2 / 19.5
+// alone on a compute unit and 14.5 / 38 the pair; 192-wide ones 12.5 / 31 where few units have one and 19.5 / 46 where all have;
+// 256-wide ones 18.5 / 51 and 26 / 70.  E.g. A for r = K = 4096, two parts: 228 us in 128-wide tiles (528 of them, two rounds), 186
+// in 192-wide (253, one round), 232 in 256-wide (136 on 256 units); r = 1024, K = 4096: 79 in one slab, 29 in four.
+double ns_rounds(int tile, int parts, double n, double ks, double units) {
+  const double k = ks / 1024;
+  if (tile == 128) {
+    const double pair = parts == 1 ? 14.5 : 38, alone = parts == 1 ? 10.2 : 19.5;
+    const double full = std::floor(n / (2 * units)), rest = n - full * 2 * units;
+    return full * (pair * k + 1) + (rest > units ? pair * k + 1 : rest > 0 ? alone * k + 1 : 0);
+  }
+  const double few = tile == 256 ? (parts == 1 ? 18.5 : 51) : (parts == 1 ? 12.5 : 31);
+  const double all = tile == 256 ? (parts == 1 ? 26 : 70) : (parts == 1 ? 19.5 : 46);
+  const double full = std::floor(n / units), rest = n / units - full;
+  return full * (all * k + 2) + (rest > 0 ? (few + (all - few) * rest) * k + 2 : 0);
+}
+
+constexpr int64_t kNsPad = 64;
+int64_t padded(int64_t n) { return ceil_div(n, kNsPad) * kNsPad; }
+
+}  // namespace
+
+// ------------------------------------------------------------------------------------------------------ norm layers
+// lanes per row and pieces per lane for a row of n elements; 0 lanes: wide
+RowShape norm_forward_shape(int64_t n, int dtype) {
+  const int64_t pieces = ceil_div(n, dtype == 0 ? 4 : 8);
+  for (int lanes = 64; lanes <= 1024; lanes *= 2)
+    if (pieces <= 2 * lanes) return {lanes, pieces <= lanes ? 1 : 2};
+  if (pieces <= 4096) return {1024, 4};
+  return {0, 0};
+}
+
+// The backward pass holds more of a row per element: eight elements a lane, sixteen of the widest rows.  With sixteen a lane the
+// registers of a bf16 row spilled: 8192 x 4096 61 us, with eight 41.
+RowShape norm_backward_shape(int64_t n, int dtype) {
+  const int pieces = dtype == 0 ? 2 : 1;
+  for (int lanes = 64; lanes <= 1024; lanes *= 2)
+    if (n <= 8 * lanes) return {lanes, pieces};
+  return n <= 16 * 1024 ? RowShape{1024, 2 * pieces} : RowShape{0, 0};
+}
+
+int64_t norm_parts(int64_t T, int64_t n, int dtype, int compute_units) {
+  const RowShape s = norm_backward_shape(n, dtype);
+  // two workgroups a compute unit (one of 1024 lanes)
+  const int64_t most = s.lanes ? (s.lanes > 512 ? 1 : 2) * (int64_t)compute_units : 64;
+  const int64_t need = ceil_div(T, s.lanes ? (s.lanes > kNormBackThreads ? 1 : kNormBackThreads / s.lanes) : 1);
+  return need < most ? need : most;
+}
+
+// ---------------------------------------------------------------------------------------------------- linear layers
+int64_t linear_parts(int64_t T, int64_t out, int dtype, int compute_units) {
+  const int64_t blocks = ceil_div(out, kGateLanes * (dtype == 0 ? 4 : 8)), need = ceil_div(T, kGateRows);
+  const int64_t want = ceil_div(4 * (int64_t)compute_units, blocks);
+  return want < 1 ? 1 : want < need ? want : need;
+}
+
+LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, int dtype, int compute_units) {
+  const int small = dtype == 0 ? 64 : 128;
+  const int64_t unit = dtype == 0 ? 32 : 64;                 // k of a stage: slabs are whole stages
+  // rows without 16-byte pieces go through registers, in small tiles (fp32 always does)
+  const bool direct = K % 8 == 0 && N % 8 == 0;
+  LinearPlan best{small, 1, K};
+  double least = -1;
+  for (int tile = small; tile <= (direct || dtype == 0 ? 2 * small : small); tile *= 2) {
+    const double tiles = (double)ceil_div(M, tile) * (double)ceil_div(N, tile);
+    for (int want = 1; want <= 16; ++want) {
+      const int64_t ks = ceil_div(ceil_div(K, want), unit) * unit;
+      const int64_t slabs = ceil_div(K, ks);
+      if (slabs != want || (want > 1 && ks < 256)) continue;
+      double cost = round_cost(dtype, tile, tiles * (double)slabs, (double)ks, compute_units);
+      if (!direct && dtype != 0) cost *= 1.6;                // 1001 x 2907 x 2705: 51 us where the direct loads' rule says 32
+      if (slabs > 1) cost += 3 + (8.0 * (double)slabs + 4) * (double)M * (double)N / 7e6;
+      if (least < 0 || cost < least) {
+        least = cost;
+        best = LinearPlan{tile, (int32_t)slabs, slabs > 1 ? ks : K};
+      }
+    }
+  }
+  return best;
+}
+
+// Up to 32 tokens: two column blocks of the matrix instruction.  4096 x 4096, 64 tokens: 16 us by tiles and slabs.
+bool linear_takes_few(int64_t T) { return T <= 32; }
+
+// ------------------------------------------------------------------------------------------- orthogonalised updates
+// Slabs only in 128-wide tiles: where they pay there are few tiles.  Joining them costs a launch and their traffic at 4.5 TB/s.
+NsCut ns_cut(int64_t r, int64_t K, int parts, int compute_units) {
+  NsCut best{128, 1, K};
+  double least = -1;
+  for (int tile : {128, 192, 256}) {
+    const double tiles = (double)ns_half_tiles(r, tile);
+    for (int slabs = 1; slabs <= (tile == 128 ? 16 : 1); ++slabs) {
+      const int64_t ks = padded(ceil_div(K, slabs));
+      if (ceil_div(K, ks) != slabs || (slabs > 1 && ks < 128)) continue;
+      double cost = ns_rounds(tile, parts, tiles * slabs, (double)ks, compute_units);
+      if (slabs > 1) cost += 3 + tiles * (slabs + 1) * 65536 / 4.5e6;
+      if (least < 0 || cost < least) {
+        least = cost;
+        best = NsCut{tile, slabs, slabs > 1 ? ks : K};
+      }
+    }
+  }
+  return best;
+}
+
+int ns_apply_tile(int64_t rows, int64_t cols, int64_t K, int parts, int compute_units) {
+  auto cost = [&](int tile) {
+    return ns_rounds(tile, parts, (double)(ceil_div(rows, tile) * ceil_div(cols, tile)), (double)K, compute_units);
+  };
+  return cost(256) < cost(128) ? 256 : 128;
+}
+
+NsLayout ns_layout(int64_t rows, int64_t cols, int parts, int compute_units) {
+  NsLayout l;
+  l.rows_p = padded(rows);
+  l.cols_p = padded(cols);
+  l.r = l.rows_p < l.cols_p ? l.rows_p : l.cols_p;
+  const int64_t c = l.rows_p < l.cols_p ? l.cols_p : l.rows_p;
+  l.x = (size_t)l.rows_p * (size_t)l.cols_p * 2u * (size_t)parts;
+  l.a = (size_t)l.r * (size_t)l.r * 2u * (size_t)parts;
+  l.sums = 0;
+  for (int64_t k : {c, l.r}) {
+    const NsCut cut = ns_cut(l.r, k, parts, compute_units);
+    const size_t need = cut.slabs > 1 ? (size_t)cut.slabs * (size_t)ns_half_tiles(l.r, cut.tile) * (size_t)(cut.tile * cut.tile) * 4u : 0;
+    if (need > l.sums) l.sums = need;
+  }
+  l.total = 256 + kNsNormBlocks * sizeof(double) + 2 * l.x + 2 * l.a + l.sums;
+  return l;
+}
+
+}  // namespace chunkft

@@ -6,8 +6,6 @@
 //   dx = dz W                          the product with W across k
 #include <hip/hip_runtime.h>
 
-#include <cmath>
-
 #include "internal.h"
 #include "launch.h"
 #include "layers.h"
@@ -252,7 +250,6 @@ __global__ __launch_bounds__(64 * kFewWaves) void linear_few_kernel(const T* X, 
 }
 
 // --------------------------------------------------------------------- dz = dy act'(z) and its sums over the tokens
-constexpr int kGateLanes = 32, kGateRows = 8;       // lanes along the columns, rows at a time
 template <typename T, bool SUMS>
 __global__ __launch_bounds__(kGateLanes * kGateRows) void gate_kernel(const T* dY, int64_t lddy, const T* Z, int64_t ldz, T* dZ,
                                                                       int64_t lddz, int64_t tokens, int64_t out, int act, float* ws,
@@ -382,58 +379,6 @@ int launch_few(const LinearProblem& p, const Epilogue& e, hipStream_t st) {
 }
 
 }  // namespace
-
-int64_t linear_parts(int64_t T, int64_t out, int dtype, int compute_units) {
-  const int64_t blocks = ceil_div(out, kGateLanes * (dtype == 0 ? 4 : 8)), need = ceil_div(T, kGateRows);
-  const int64_t want = ceil_div(4 * (int64_t)compute_units, blocks);
-  return want < 1 ? 1 : want < need ? want : need;
-}
-
-// What a cut costs, in us, from rounds of workgroups (n items of a tile with ks values of k each on so many compute units) and the
-// slabs' traffic.  Measured per 1024 k (and 1 - 2 us around them): bf16, 256-wide tiles, one to a unit, 19.5 where few units have
-// one and 24 where all have; 128-wide ones 10.2 alone on a unit, 14.5 the pair.  fp32: 22 and 18.2 for 64-wide ones alone and
-// each of several, 72 and 64.5 for 128-wide ones.  Slabs: 8 bytes per slab and element at 7 TB/s, and a launch.
-// E.g. bf16, 4096 x 4096 x 14336: 256-wide tiles 388 us, 128-wide 419; 512 x 14336 x 4096 one slab of 128-wide tiles 146, four 64;
-// 1024 x 14336 x 4096 162 and, four slabs of 256-wide tiles, 108.
-double round_cost(int dtype, int tile, double items, double ks, double units) {
-  const double k = ks / 1024;
-  if (dtype == 0) {
-    const double each = std::ceil(items / units);
-    return tile == 64 ? (each <= 1 ? 22 : 18.2 * each) * k : (each <= 1 ? 72 : 64.5 * each) * k;
-  }
-  if (tile == 256) {
-    const double full = std::floor(items / units), rest = items / units - full;
-    return full * (24 * k + 2) + (rest > 0 ? (19.5 + 4.5 * rest) * k + 2 : 0);
-  }
-  const double full = std::floor(items / (2 * units)), rest = items - full * 2 * units;
-  return full * (14.5 * k + 1) + (rest > units ? 14.5 * k + 1 : rest > 0 ? 10.2 * k + 1 : 0);
-}
-
-LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, int dtype, int compute_units) {
-  const int small = dtype == 0 ? 64 : 128;
-  const int64_t unit = dtype == 0 ? 32 : 64;                 // k of a stage: slabs are whole stages
-  // rows without 16-byte pieces go through registers, in small tiles (fp32 always does)
-  const bool direct = K % 8 == 0 && N % 8 == 0;
-  LinearPlan best{small, 1, K};
-  double least = -1;
-  for (int tile = small; tile <= (direct || dtype == 0 ? 2 * small : small); tile *= 2) {
-    const double tiles = (double)ceil_div(M, tile) * (double)ceil_div(N, tile);
-    for (int want = 1; want <= 16; ++want) {
-      const int64_t ks = ceil_div(ceil_div(K, want), unit) * unit;
-      const int64_t slabs = ceil_div(K, ks);
-      if (slabs != want || (want > 1 && ks < 256)) continue;
-      double cost = round_cost(dtype, tile, tiles * (double)slabs, (double)ks, compute_units);
-      if (!direct && dtype != 0) cost *= 1.6;                // 1001 x 2907 x 2705: 51 us where the direct loads' rule says 32
-      if (slabs > 1) cost += 3 + (8.0 * (double)slabs + 4) * (double)M * (double)N / 7e6;
-      if (least < 0 || cost < least) {
-        least = cost;
-        best = LinearPlan{tile, (int32_t)slabs, slabs > 1 ? ks : K};
-      }
-    }
-  }
-  return best;
-}
-bool linear_takes_few(int64_t T) { return T <= 32; }
 
 int launch_linear_forward(const LinearProblem& p, void* Y, int64_t ldy, void* Z, int64_t ldz, float* ws, void* stream) {
   hipStream_t st = (hipStream_t)stream;

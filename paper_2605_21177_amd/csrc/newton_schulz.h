@@ -28,17 +28,6 @@ struct NsBuffers {
   unsigned short* poly;
   float* sums;                     // slabs of A's and the polynomial's tiles
 };
-constexpr int64_t kNsPad = 64;
-
-// How the product of an r x r result over K is cut: tiles of its lower half, slabs of kslab values of k.
-struct NsCut {
-  int32_t tile, slabs;
-  int64_t kslab;
-};
-NsCut ns_cut(int64_t r, int64_t K, int parts, int compute_units);
-int ns_apply_tile(int64_t rows, int64_t cols, int64_t K, int parts, int compute_units);
-inline int64_t ns_half_tiles(int64_t r, int tile) { const int64_t n = ceil_div(r, tile); return n * (n + 1) / 2; }
-
 template <int NP> int run_newton_schulz(const OrthoProblem& p, const NsBuffers& b, hipStream_t st);
 
 typedef __attribute__((ext_vector_type(8))) _Float16 h8;

@@ -169,7 +169,7 @@ __global__ __launch_bounds__(kWideThreads) void norm_forward_wide_kernel(const N
 // before the present ones are finished.  At the end its R groups meet in LDS, in order, and leave one partial row of each sum.
 // 8192 tokens x 4096, bf16: 41 us, 4.9 TB/s (82 without the request ahead, one workgroup a unit, and conversions in integer arithmetic;
 // without the sums 33).
-template <int G> constexpr int kBackThreads = G > 512 ? G : 512;
+template <int G> constexpr int kBackThreads = G > kNormBackThreads ? G : kNormBackThreads;
 
 template <typename T, int SUB, int G, int PC, bool SUMS, bool EXACT>
 __global__ __launch_bounds__(kBackThreads<G>, 4) void norm_backward_kernel(const NormProblem p, const NormGrads g, float* ws, int64_t pitch) {
@@ -386,18 +386,8 @@ __global__ __launch_bounds__(kSumCols * kSumLanes) void sum_parts_kernel(const f
   if (k == 0 && i < t.count) t.out[i] = accumulate ? t.out[i] + red[0][c] : red[0][c];
 }
 
-// lanes per row and pieces per lane for a row of n elements; 0 lanes: wide
-struct Shape { int lanes, pieces; };
-Shape shape_of(int64_t n, int dtype) {
-  const int64_t pieces = ceil_div(n, dtype == 0 ? 4 : 8);
-  for (int lanes = 64; lanes <= 1024; lanes *= 2)
-    if (pieces <= 2 * lanes) return {lanes, pieces <= lanes ? 1 : 2};
-  if (pieces <= 4096) return {1024, 4};
-  return {0, 0};
-}
-
 template <class F>
-int with_shape(const Shape& s, F&& f) {
+int with_shape(const RowShape& s, F&& f) {
   if (s.pieces == 4) return f(IntC<1024>{}, IntC<4>{});
   switch (s.lanes) {
     case 64: return s.pieces == 1 ? f(IntC<64>{}, IntC<1>{}) : f(IntC<64>{}, IntC<2>{});
@@ -408,17 +398,8 @@ int with_shape(const Shape& s, F&& f) {
   }
 }
 
-// The backward pass holds more of a row per element: eight elements a lane, sixteen of the widest rows.  With sixteen a lane the
-// registers of a bf16 row spilled: 8192 x 4096 61 us, with eight 41.
-Shape backward_shape_of(int64_t n, int dtype) {
-  const int pieces = dtype == 0 ? 2 : 1;
-  for (int lanes = 64; lanes <= 1024; lanes *= 2)
-    if (n <= 8 * lanes) return {lanes, pieces};
-  return n <= 16 * 1024 ? Shape{1024, 2 * pieces} : Shape{0, 0};
-}
-
 template <typename T, class F>
-int with_backward_shape(const Shape& s, F&& f) {
+int with_backward_shape(const RowShape& s, F&& f) {
   constexpr int PC = 8 / Row<T>::N;
   if (s.pieces != PC) return f(IntC<1024>{}, IntC<2 * PC>{});
   switch (s.lanes) {
@@ -430,11 +411,9 @@ int with_backward_shape(const Shape& s, F&& f) {
   }
 }
 
-int rows_at_once(const Shape& s) { return s.lanes > 512 ? 1 : 512 / s.lanes; }
-
 template <typename T, int SUB>
 int forward_typed(const NormProblem& p, int dtype, void* Y, int64_t ldy, float* stats, hipStream_t st) {
-  const Shape s = shape_of(p.n, dtype);
+  const RowShape s = norm_forward_shape(p.n, dtype);
   if (!s.lanes) {
     if (p.T > kMaxLaunchThreads / kWideThreads) return (int)hipErrorInvalidValue;
     hipLaunchKernelGGL((norm_forward_wide_kernel<T, SUB>), dim3((unsigned)p.T), dim3(kWideThreads), 0, st, p, (T*)Y, ldy, stats);
@@ -451,7 +430,7 @@ int forward_typed(const NormProblem& p, int dtype, void* Y, int64_t ldy, float* 
 
 template <typename T, int SUB>
 int backward_typed(const NormProblem& p, int dtype, const NormGrads& g, float* ws, hipStream_t st) {
-  const Shape s = backward_shape_of(p.n, dtype);
+  const RowShape s = norm_backward_shape(p.n, dtype);
   const bool sums = g.dw || g.db;
   const int64_t parts = norm_parts(p.T, p.n, dtype, device_compute_units()), pitch = norm_pitch(p.n);
   if (!s.lanes) {
@@ -483,14 +462,6 @@ int backward_typed(const NormProblem& p, int dtype, const NormGrads& g, float* w
 }
 
 }  // namespace
-
-int64_t norm_parts(int64_t T, int64_t n, int dtype, int compute_units) {
-  const Shape s = backward_shape_of(n, dtype);
-  // two workgroups a compute unit (one of 1024 lanes)
-  const int64_t most = s.lanes ? (s.lanes > 512 ? 1 : 2) * (int64_t)compute_units : 64;
-  const int64_t need = ceil_div(T, s.lanes ? rows_at_once(s) : 1);
-  return need < most ? need : most;
-}
 
 int launch_sum_parts(const float* ws, int64_t parts, int64_t stride, const SumTarget& t0, const SumTarget& t1, int accumulate,
                      void* stream) {

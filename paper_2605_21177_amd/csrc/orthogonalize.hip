@@ -14,15 +14,11 @@
 // The matrices are padded with zeros to multiples of 64, whole stages of the products' k, and the steps keep the zeros.
 #include <hip/hip_runtime.h>
 
-#include <cmath>
-
 #include "newton_schulz_steps.h"
 
 namespace chunkft {
 
 namespace {
-
-constexpr int kNormBlocks = 1024;                // most partial sums of the norm
 
 // ------------------------------------------------------------------------------ momentum, norm, parts
 // G as `lines` lines of `len` elements: a matrix without padding is one line.
@@ -130,37 +126,13 @@ __global__ __launch_bounds__(256) void hold_kernel(const T* G, int64_t ldg, cons
   }
 }
 
-int64_t padded(int64_t n) { return (n + kNsPad - 1) / kNsPad * kNsPad; }
-
-struct Layout {
-  int64_t rows_p, cols_p, r;        // r: padded small side
-  size_t x, a, sums, total;         // bytes of a buffer of X, of A, of the slabs' sums, of all
-};
-Layout layout_of(int64_t rows, int64_t cols, int parts) {
-  Layout l;
-  l.rows_p = padded(rows);
-  l.cols_p = padded(cols);
-  l.r = l.rows_p < l.cols_p ? l.rows_p : l.cols_p;
-  const int64_t c = l.rows_p < l.cols_p ? l.cols_p : l.rows_p;
-  l.x = (size_t)l.rows_p * (size_t)l.cols_p * 2u * (size_t)parts;
-  l.a = (size_t)l.r * (size_t)l.r * 2u * (size_t)parts;
-  l.sums = 0;
-  for (int64_t k : {c, l.r}) {
-    const NsCut cut = ns_cut(l.r, k, parts, device_compute_units());
-    const size_t need = cut.slabs > 1 ? (size_t)cut.slabs * (size_t)ns_half_tiles(l.r, cut.tile) * (size_t)(cut.tile * cut.tile) * 4u : 0;
-    if (need > l.sums) l.sums = need;
-  }
-  l.total = 256 + kNormBlocks * sizeof(double) + 2 * l.x + 2 * l.a + l.sums;
-  return l;
-}
-
 template <typename T>
-int prepare(const OrthoProblem& p, const Layout& l, double* parts, NsScalars* sc, unsigned short* x, hipStream_t st) {
+int prepare(const OrthoProblem& p, const NsLayout& l, double* parts, NsScalars* sc, unsigned short* x, hipStream_t st) {
   Source s{p.G, p.ldg, p.rows, p.cols, p.m, p.momentum, p.nesterov};
   if (p.ldg == p.cols) s.lines = 1, s.len = p.rows * p.cols;
   const int64_t across = ceil_div(s.len, 256 * Row<T>::N);
-  const int gx = (int)(across < kNormBlocks ? across : kNormBlocks);
-  const int64_t room = kNormBlocks / gx;
+  const int gx = (int)(across < kNsNormBlocks ? across : kNsNormBlocks);
+  const int64_t room = kNsNormBlocks / gx;
   const int gy = (int)(s.lines < room ? s.lines : room);
   hipLaunchKernelGGL((momentum_norm_kernel<T>), dim3(gx, gy), dim3(256), 0, st, s, parts);
   hipLaunchKernelGGL(scalars_kernel, dim3(1), dim3(256), 0, st, parts, gx * gy, p.eps, sc);
@@ -177,55 +149,9 @@ int prepare(const OrthoProblem& p, const Layout& l, double* parts, NsScalars* sc
 
 extern template int run_newton_schulz<2>(const OrthoProblem& p, const NsBuffers& b, hipStream_t st);   // orthogonalize_two.hip
 
-// Time in us of `n` workgroups of a tile with ks values of k each.  Measured per 1024 k, one part / two: 128-wide tiles 10.2 / 19.5
-// alone on a compute unit and 14.5 / 38 the pair; 192-wide ones 12.5 / 31 where few units have one and 19.5 / 46 where all have;
-// 256-wide ones 18.5 / 51 and 26 / 70.  E.g. A for r = K = 4096, two parts: 228 us in 128-wide tiles (528 of them, two rounds), 186
-// in 192-wide (253, one round), 232 in 256-wide (136 on 256 units); r = 1024, K = 4096: 79 in one slab, 29 in four.
-double ns_rounds(int tile, int parts, double n, double ks, double units) {
-  const double k = ks / 1024;
-  if (tile == 128) {
-    const double pair = parts == 1 ? 14.5 : 38, alone = parts == 1 ? 10.2 : 19.5;
-    const double full = std::floor(n / (2 * units)), rest = n - full * 2 * units;
-    return full * (pair * k + 1) + (rest > units ? pair * k + 1 : rest > 0 ? alone * k + 1 : 0);
-  }
-  const double few = tile == 256 ? (parts == 1 ? 18.5 : 51) : (parts == 1 ? 12.5 : 31);
-  const double all = tile == 256 ? (parts == 1 ? 26 : 70) : (parts == 1 ? 19.5 : 46);
-  const double full = std::floor(n / units), rest = n / units - full;
-  return full * (all * k + 2) + (rest > 0 ? (few + (all - few) * rest) * k + 2 : 0);
-}
-
-// Slabs only in 128-wide tiles: where they pay there are few tiles.  Joining them costs a launch and their traffic at 4.5 TB/s.
-NsCut ns_cut(int64_t r, int64_t K, int parts, int compute_units) {
-  NsCut best{128, 1, K};
-  double least = -1;
-  for (int tile : {128, 192, 256}) {
-    const double tiles = (double)ns_half_tiles(r, tile);
-    for (int slabs = 1; slabs <= (tile == 128 ? 16 : 1); ++slabs) {
-      const int64_t ks = padded(ceil_div(K, slabs));
-      if (ceil_div(K, ks) != slabs || (slabs > 1 && ks < 128)) continue;
-      double cost = ns_rounds(tile, parts, tiles * slabs, (double)ks, compute_units);
-      if (slabs > 1) cost += 3 + tiles * (slabs + 1) * 65536 / 4.5e6;
-      if (least < 0 || cost < least) {
-        least = cost;
-        best = NsCut{tile, slabs, slabs > 1 ? ks : K};
-      }
-    }
-  }
-  return best;
-}
-
-int ns_apply_tile(int64_t rows, int64_t cols, int64_t K, int parts, int compute_units) {
-  auto cost = [&](int tile) {
-    return ns_rounds(tile, parts, (double)(ceil_div(rows, tile) * ceil_div(cols, tile)), (double)K, compute_units);
-  };
-  return cost(256) < cost(128) ? 256 : 128;
-}
-
-size_t ortho_workspace_bytes(int64_t rows, int64_t cols, int parts) { return layout_of(rows, cols, parts).total; }
-
 int launch_orthogonalize(const OrthoProblem& p, void* ws, void* stream) {
   hipStream_t st = (hipStream_t)stream;
-  const Layout l = layout_of(p.rows, p.cols, p.parts);
+  const NsLayout l = ns_layout(p.rows, p.cols, p.parts, device_compute_units());
   unsigned char* at = (unsigned char*)ws;
   auto take = [&](size_t bytes) {
     unsigned char* const q = at;
@@ -233,7 +159,7 @@ int launch_orthogonalize(const OrthoProblem& p, void* ws, void* stream) {
     return q;
   };
   NsScalars* const sc = (NsScalars*)take(256);
-  double* const parts = (double*)take(kNormBlocks * sizeof(double));
+  double* const parts = (double*)take(kNsNormBlocks * sizeof(double));
   NsBuffers b{l.rows_p, l.cols_p, l.r, sc};
   b.x0 = (unsigned short*)take(l.x);
   b.x1 = (unsigned short*)take(l.x);
