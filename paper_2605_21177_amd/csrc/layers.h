@@ -86,7 +86,7 @@ struct LinearPlan {
   int64_t kslab;
 };
 LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, int dtype, int compute_units);
-bool linear_takes_few(int64_t T);        // the forward pass reads the weights once, whatever the plan
+bool linear_takes_few(int64_t T, int64_t out, int64_t in, int dtype);   // the forward pass is one pass over the weights, whatever the plan
 
 int launch_linear_forward(const LinearProblem& p, void* Y, int64_t ldy, void* Z, int64_t ldz, float* ws, void* stream);
 int launch_linear_backward(const LinearProblem& p, const LinearGrads& g, float* ws, void* stream);

@@ -74,7 +74,7 @@ size_t slab_need(int64_t M, int64_t N, int64_t K, int32_t dtype) {
   return plan.slabs <= 1 ? 0 : static_cast<size_t>(plan.slabs) * static_cast<size_t>(M) * static_cast<size_t>(norm_pitch(N)) * 4u;
 }
 
-size_t forward_need(const LinearProblem& p) { return linear_takes_few(p.T) ? 0 : slab_need(p.T, p.out, p.in, p.dtype); }
+size_t forward_need(const LinearProblem& p) { return linear_takes_few(p.T, p.out, p.in, p.dtype) ? 0 : slab_need(p.T, p.out, p.in, p.dtype); }
 
 // The bias' partial sums are done with when the product's begin: one after the other on the stream they share the space.
 size_t backward_need(const LinearProblem& p, bool bias, bool input) {

@@ -112,8 +112,17 @@ LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, int dtype, int compute_u
   return best;
 }
 
-// Up to 32 tokens: two column blocks of the matrix instruction.  4096 x 4096, 64 tokens: 16 us by tiles and slabs.
-bool linear_takes_few(int64_t T) { return T <= 32; }
+// The pass over the weights against tiles and slabs: x is read again by every workgroup, and rows that are no 16-byte pieces in twice
+// the requests.  bf16, us, pass / tiles: 1 token 4096 x 14336 25 / 47, 8 tokens 28 / 29, 16 tokens 34 / 28, 16 tokens 4096 x 4096
+// 11 / 16, 16 tokens 8192 x 8192 37 / 32, 32 tokens 4096 x 4096 13 / 17, 4096 x 6144 25 / 18; rows without pieces 1 token
+// 4095 x 4097 19 / 20, 4095 x 14337 58 / 40, 4 tokens 1001 x 1003 7 / 12; fp32 16 tokens 4096 x 14336 67 / 80, 32 tokens 96 / 82.
+bool linear_takes_few(int64_t T, int64_t out, int64_t in, int dtype) {
+  const double weights = (double)out * (double)in, M = 1 << 20;
+  if (T > 32) return false;
+  if (dtype != 0 && in % 8 != 0) return T <= 16 && (double)T * weights <= 32 * M;
+  if (T > 16) return weights <= 16 * M;
+  return T <= 8 || dtype == 0 || weights <= 32 * M;
+}
 
 // ------------------------------------------------------------------------------------------- orthogonalised updates
 // Slabs only in 128-wide tiles: where they pay there are few tiles.  Joining them costs a launch and their traffic at 4.5 TB/s.

@@ -103,7 +103,7 @@ __device__ __forceinline__ P slab_of(P q, const Slabs& s, int slab) {
   return q;
 }
 
-template <class C, int KB, bool DMA, bool SPLIT>
+template <class C, int KB, int HOW, bool SPLIT>
 __global__ __launch_bounds__(C::NT, 2) void linear_kernel(const Product whole, const TileOrder o, int n_items, const Epilogue e,
                                                                 const Slabs s) {
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
@@ -114,7 +114,7 @@ __global__ __launch_bounds__(C::NT, 2) void linear_kernel(const Product whole, c
   tile_at(o, item - slab * tiles, tm, tn);
   const Product q = SPLIT ? slab_of<Product, KB>(whole, s, slab) : whole;
   const int64_t row0 = (int64_t)tm * C::BM, col0 = (int64_t)tn * C::BN;
-  product_tile<C, 0, KB, false, DMA>(q, row0, col0, lds, [&](int m, int n, float (&v)[8]) {
+  product_tile<C, 0, KB, false, HOW>(q, row0, col0, lds, [&](int m, int n, float (&v)[8]) {
     const int64_t r = row0 + m, c = col0 + n;
     if (r >= q.M || c >= q.N) return;
     if constexpr (SPLIT) {                        // the pitch is a multiple of 8: whole pieces
@@ -173,9 +173,10 @@ __global__ __launch_bounds__(256) void join_slabs_kernel(const Slabs s, int64_t 
 }
 
 // ------------------------------------------------------------------------------------------------ few tokens
-// Up to 16 NB tokens: the weights are read once and nothing else counts.  A workgroup has 16 rows of W; its eight waves take pieces
-// of 128 bytes of them in turn, straight from memory into the registers of the matrix instruction (a lane has 16 bytes of one
-// row), against the same k of x, which stay in the caches.  The eight sums meet in LDS, in order.
+// Up to 16 NB tokens: the weights are read once and little else counts.  A workgroup has 16 rows of W; its eight waves take pieces
+// of 64 bytes of them in turn, straight from memory into the registers of the matrix instruction (a lane has 16 bytes of one
+// row), against the same k of x, which stay in the caches.  The eight sums meet in LDS, in order.  One token, 4096 x 14336: 25 us,
+// 4.7 TB/s.  (32 rows a workgroup read x half as often: 30 us there, 33 instead of 34 at 16 tokens.)
 template <typename T> struct FewStep;
 template <> struct FewStep<unsigned short> {
   static constexpr int K = 32;                   // of an instruction group
@@ -318,14 +319,14 @@ bool fill_order(int64_t M, int64_t N, int64_t bm, int64_t bn, int threads, int s
 typedef ProductCfg<256, 256, 4, 2, 3, 2> Tile256;
 typedef ProductCfg<128, 128, 2, 2, 2, 2> Tile128;
 
-template <class C, int KB, bool DMA, bool SPLIT>
+template <class C, int KB, int HOW, bool SPLIT>
 int launch_tiles(const Product& q, const Epilogue& e, const Slabs& s, hipStream_t st) {
   TileOrder o;
   int n;
   if (!fill_order(q.M, q.N, C::BM, C::BN, C::NT, s.count, o, n)) return (int)hipErrorInvalidValue;
-  const int err = raise_lds_limit<linear_kernel<C, KB, DMA, SPLIT>>(C::LDS);
+  const int err = raise_lds_limit<linear_kernel<C, KB, HOW, SPLIT>>(C::LDS);
   if (err != 0) return err;
-  hipLaunchKernelGGL((linear_kernel<C, KB, DMA, SPLIT>), dim3((unsigned)((n + 7) / 8 * 8)), dim3(C::NT), C::LDS, st, q, o, n, e, s);
+  hipLaunchKernelGGL((linear_kernel<C, KB, HOW, SPLIT>), dim3((unsigned)((n + 7) / 8 * 8)), dim3(C::NT), C::LDS, st, q, o, n, e, s);
   return (int)hipGetLastError();
 }
 
@@ -358,14 +359,19 @@ int launch_product(const void* A, int64_t lda, const void* B, int64_t ldb, int64
     return err != 0 || plan.slabs == 1 ? err : join_slabs<float>(s, M, N, e, st);
   }
   const Product q{(const unsigned short*)A, (const unsigned short*)B, lda, ldb, M, N, K};
-  const bool direct = direct_rows(A, lda, K, false) && direct_rows(B, ldb, N, KB != 0);
-  if (plan.slabs > 1) {
-    if (!direct) err = launch_tiles<Tile128, KB, false, true>(q, e, s, st);
-    else err = plan.tile == 256 ? launch_tiles<Tile256, KB, true, true>(q, e, s, st) : launch_tiles<Tile128, KB, true, true>(q, e, s, st);
-    return err != 0 ? err : join_slabs<unsigned short>(s, M, N, e, st);
-  }
-  if (!direct) return launch_tiles<Tile128, KB, false, false>(q, e, s, st);
-  return plan.tile == 256 ? launch_tiles<Tile256, KB, true, false>(q, e, s, st) : launch_tiles<Tile128, KB, true, false>(q, e, s, st);
+  // a slab of fewer k than a stage has nothing for the direct loads
+  const int64_t last = plan.slabs > 1 ? K - (plan.slabs - 1) * plan.kslab : K;
+  const bool direct = direct_rows(A, lda, K, false) && direct_rows(B, ldb, N, KB != 0) && last >= Tile128::BK;
+  auto by_split = [&](auto split) {
+    constexpr bool S = decltype(split)::value != 0;
+    if (!direct) return launch_tiles<Tile128, KB, THROUGH_REGISTERS, S>(q, e, s, st);
+    if (K % Tile128::BK == 0)
+      return plan.tile == 256 ? launch_tiles<Tile256, KB, DIRECT, S>(q, e, s, st) : launch_tiles<Tile128, KB, DIRECT, S>(q, e, s, st);
+    return plan.tile == 256 ? launch_tiles<Tile256, KB, DIRECT_AND_TAIL, S>(q, e, s, st) : launch_tiles<Tile128, KB, DIRECT_AND_TAIL, S>(q, e, s, st);
+  };
+  if (plan.slabs == 1) return by_split(IntC<0>{});
+  err = by_split(IntC<1>{});
+  return err != 0 ? err : join_slabs<unsigned short>(s, M, N, e, st);
 }
 
 template <typename T>
@@ -383,7 +389,7 @@ int launch_few(const LinearProblem& p, const Epilogue& e, hipStream_t st) {
 int launch_linear_forward(const LinearProblem& p, void* Y, int64_t ldy, void* Z, int64_t ldz, float* ws, void* stream) {
   hipStream_t st = (hipStream_t)stream;
   const Epilogue e{p.bias, p.residual, Y, Z, p.ldr, ldy, ldz, p.act};
-  if (linear_takes_few(p.T)) return p.dtype == 0 ? launch_few<float>(p, e, st) : launch_few<unsigned short>(p, e, st);
+  if (linear_takes_few(p.T, p.out, p.in, p.dtype)) return p.dtype == 0 ? launch_few<float>(p, e, st) : launch_few<unsigned short>(p, e, st);
   return launch_product<0>(p.X, p.ldx, p.W, p.ldw, p.T, p.out, p.in, p.dtype, e, ws, st);
 }
 

@@ -132,7 +132,7 @@ __global__ __launch_bounds__(C::NT, 2) void step_kernel(const StepArgs s) {
   };
   if constexpr (HALF && !SPLIT) {
     // the other half, by its own rows: one value of A for both, so the two are alike to the bit
-    product_tile<C, KA, KB, true, true>(q, row0, col0, lds, put, [&](int m, int n, float (&v)[16]) {
+    product_tile<C, KA, KB, true, DIRECT>(q, row0, col0, lds, put, [&](int m, int n, float (&v)[16]) {
       const int64_t r = col0 + n, c = row0 + m;
       if (tm == tn || r >= q.N || c >= q.M) return;
 #pragma unroll
@@ -145,7 +145,7 @@ __global__ __launch_bounds__(C::NT, 2) void step_kernel(const StepArgs s) {
       }
     });
   } else {
-    product_tile<C, KA, KB, true, true>(q, row0, col0, lds, put);
+    product_tile<C, KA, KB, true, DIRECT>(q, row0, col0, lds, put);
   }
 }
 

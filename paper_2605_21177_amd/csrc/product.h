@@ -2,9 +2,9 @@
 //
 // Either operand lies with k along its rows, [m][k] and [n][k], or across them, [k][m] and [k][n] (KA, KB).  A stage of BK
 // values of k of both travels from memory into one of the slots of two rings in LDS:
-//   DMA   16-byte rows and enough of them: loads that write LDS directly, a scalar base and a constant per-lane offset
-//   else  through registers, 16 bytes at any 2-byte address, element by element at the ends of the rows; also the last, partial
-//         stage of the other form, where what lies past k is stored as zero in both operands
+//   16-byte rows: loads that write LDS directly, a scalar base and a constant per-lane offset
+//   others: through registers, 16 bytes at any 2-byte address, element by element at the ends of the rows; also the last, partial
+//   stage of the other form, where what lies past k is stored as zero in both operands
 // The 16-byte pieces of a row are permuted by the row so that the reads are free of bank conflicts: rows along k are read 16 at
 // a time (ds_read_b128: piece ^ bits of the row above those that fill 256 bytes), rows across k by the transpose read, four k of
 // 16 columns per 16 lanes (piece ^ bits 0, 1 and 3 of k, in units of two pieces).
@@ -85,7 +85,7 @@ __device__ __forceinline__ f32x4 mfma16(s16x8 a, s16x8 b, f32x4 c) {
 }
 
 // Stages of an operand: the rows along k (KS = 0) or across it (KS = 1), R = rows or columns of the tile.
-template <class C, int R, int KS, bool DMA>
+template <class C, int R, int KS>
 struct Fetcher {
   static constexpr int BK = C::BK, P = KS ? R * C::NP / 8 : 8;      // pieces per row in LDS
   static constexpr int ROWS = KS ? BK : R;                          // rows in LDS
@@ -104,14 +104,12 @@ struct Fetcher {
     ld = ld_; K = K_;
     left = (total - first) * (KS ? C::NP : 1);
     base = KS ? p + first * C::NP : p + first * ld;
-    if constexpr (DMA) {
 #pragma unroll
-      for (int i = 0; i < LOADS; ++i) {
-        const int row = row_of(i, wave, lane), piece = piece_of(i, wave, lane);
-        // rows (columns) that are not there repeat the tile's first ones: their results are not stored
-        if constexpr (KS) voff[i] = (unsigned)(row * ld * 2) + (piece * 8 < left ? (unsigned)piece * 16u : 0u);
-        else voff[i] = (row < left ? (unsigned)(row * ld * 2) : 0u) + (unsigned)piece * 16u;
-      }
+    for (int i = 0; i < LOADS; ++i) {
+      const int row = row_of(i, wave, lane), piece = piece_of(i, wave, lane);
+      // rows (columns) that are not there repeat the tile's first ones: their results are not stored
+      if constexpr (KS) voff[i] = (unsigned)(row * ld * 2) + (piece * 8 < left ? (unsigned)piece * 16u : 0u);
+      else voff[i] = (row < left ? (unsigned)(row * ld * 2) : 0u) + (unsigned)piece * 16u;
     }
   }
   // Load i of a whole stage kt, straight into LDS.
@@ -185,6 +183,9 @@ struct Reader {
   }
 };
 
+// How a stage comes to LDS.  DIRECT: k is whole stages, at least one; DIRECT_AND_TAIL: at least one, and a partial one may follow.
+enum Fetch : int { THROUGH_REGISTERS = 0, DIRECT = 1, DIRECT_AND_TAIL = 2 };
+
 struct NotTurned {
   __device__ __forceinline__ void operator()(int, int, float (&)[16]) const {}
 };
@@ -192,14 +193,14 @@ struct NotTurned {
 // One tile.  put(m, n, v): the results of the tile's row m, columns n .. n + 7, whether the matrix reaches that far or not.
 // turned(m, n, v), if there is one: those of the column n, rows m .. m + 15.
 // lds: C::LDS bytes, 16-byte aligned.
-template <class C, int KA, int KB, bool F16, bool DMA, class Put, class Turned = NotTurned>
+template <class C, int KA, int KB, bool F16, int HOW, class Put, class Turned = NotTurned>
 __device__ __forceinline__ void product_tile(const Product& q, int64_t row0, int64_t col0, unsigned char* lds, Put&& put,
                                              Turned&& turned = NotTurned{}) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm0 = (wave / C::WN) * (C::BM / C::WM), wn0 = (wave % C::WN) * (C::BN / C::WN);
-  static_assert(DMA || C::NP == 1, "matrices of two parts are whole stages of 16-byte rows");
-  typedef Fetcher<C, C::BM, KA, DMA> FetchA;
-  typedef Fetcher<C, C::BN, KB, DMA> FetchB;
+  static_assert(HOW == DIRECT || C::NP == 1, "matrices of two parts are whole stages of 16-byte rows");
+  typedef Fetcher<C, C::BM, KA> FetchA;
+  typedef Fetcher<C, C::BN, KB> FetchB;
   FetchA fa;
   FetchB fb;
   fa.init(q.A, q.lda, row0, q.M, q.K, wave, lane);
@@ -209,13 +210,15 @@ __device__ __forceinline__ void product_tile(const Product& q, int64_t row0, int
   ra.init(wm0, lane);
   rb.init(wn0, lane);
   const unsigned lds_base = (unsigned)(uintptr_t)lds;
-  // the stages that the loop takes; with direct loads a partial one may follow
-  const int nk = (int)((q.K + C::BK - 1) / C::BK), loop = DMA ? (int)(q.K / C::BK) : nk;
+  // stages, and how many of them the direct loads can take (all but a partial last one)
+  const int nk = (int)((q.K + C::BK - 1) / C::BK), whole = (int)(q.K / C::BK);
   unsigned char* const ldsA = lds;
   unsigned char* const ldsB = lds + C::RING_A;
   constexpr int LA = FetchA::LOADS, LB = FetchB::LOADS;
-  auto fetch_a = [&](int j, int kt) { fa.direct(j, kt, lds_base + (unsigned)(kt % C::NSA) * C::SLOT_A, wave); };
-  auto fetch_b = [&](int j, int kt) { fb.direct(j, kt, lds_base + C::RING_A + (unsigned)(kt % C::NSB) * C::SLOT_B, wave); };
+  // Behind the last whole stage the direct loads go on, into slots that nobody reads again: the loop has no branch and always the
+  // same number of loads in flight.
+  auto fetch_a = [&](int j, int kt) { fa.direct(j, kt < whole ? kt : whole - 1, lds_base + (unsigned)(kt % C::NSA) * C::SLOT_A, wave); };
+  auto fetch_b = [&](int j, int kt) { fb.direct(j, kt < whole ? kt : whole - 1, lds_base + C::RING_A + (unsigned)(kt % C::NSB) * C::SLOT_B, wave); };
   u32x4_t va[LA], vb[LB];
   auto load = [&](int kt) {
     fa.load(kt, wave, lane, va);
@@ -225,13 +228,12 @@ __device__ __forceinline__ void product_tile(const Product& q, int64_t row0, int
     fa.store(ldsA + (kt % C::NSA) * C::SLOT_A, wave, lane, va);
     fb.store(ldsB + (kt % C::NSB) * C::SLOT_B, wave, lane, vb);
   };
-  // Every wave's part of stage kt is in LDS, and every wave has its fragments of the stage before.
-  auto arrive = [&](int kt) {
+  // Every wave's part of the next stage is in LDS, and every wave has its fragments of this one.
+  auto arrive = [&](auto aheadc) {
     __builtin_amdgcn_sched_barrier(0);
     asm volatile("" ::: "memory");
-    if (!DMA) wait_lds_and<63>();
-    else if (kt + C::MANY - 2 < loop) wait_lds_and<(C::NSA - 2) * LA + (C::NSB - 2) * LB>();
-    else wait_lds_and<0>();
+    if constexpr (decltype(aheadc)::value) wait_lds_and<(C::NSA - 2) * LA + (C::NSB - 2) * LB>();
+    else wait_lds_and<63>();
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
   };
@@ -263,20 +265,17 @@ __device__ __forceinline__ void product_tile(const Product& q, int64_t row0, int
       __builtin_amdgcn_sched_barrier(0);
     });
   };
-  // The last phase of stage kt.  turn(), which makes room, lies behind its first blocks, so that the reads of the phase before have
-  // arrived.  MORE: there is a next stage, whose first fragments are read, A's to `next`.  FETCH 2: the stages ahead of both
-  // operands are requested, 1: of the one with fewer slots, 0: none.
-  auto last_phase = [&](const s16x8 (&a_)[C::TM], auto morec, auto fetchc, int kt, s16x8 (&next)[C::TM], auto&& turn) {
-    constexpr int MORE = decltype(morec)::value, FETCH = decltype(fetchc)::value, TURN = C::TURN, MF = C::TM * C::TN;
-    constexpr int first = C::B_FIRST ? LB : LA, loads = FETCH == 2 ? LA + LB : FETCH == 1 ? first : 0;
+  // The last phase of stage kt.  The barrier, which makes room, lies behind its first blocks, so that the reads of the phase before
+  // have arrived.  Then the first fragments of the next stage are read (A's to `next`) and, with AHEAD, stages ahead are requested,
+  // a load between two matrix instructions: all at once they would hold up the matrix cores behind the barrier.
+  auto last_phase = [&](const s16x8 (&a_)[C::TM], auto aheadc, int kt, s16x8 (&next)[C::TM]) {
+    constexpr int TURN = C::TURN, MF = C::TM * C::TN, first = C::B_FIRST ? LB : LA, loads = decltype(aheadc)::value ? LA + LB : 0;
     static_assert(loads <= MF - TURN * C::TM, "a load per matrix instruction");
     static_for<TURN * C::TM>([&](auto ic) { mul(a_, ic); });
-    turn();
-    if constexpr (MORE) {
-      read_a(next, IntC<0>{}, kt + 1);
+    arrive(aheadc);
+    read_a(next, IntC<0>{}, kt + 1);
 #pragma unroll
-      for (int b = 0; b < TURN; ++b) read_b(b, IntC<0>{}, kt + 1);
-    }
+    for (int b = 0; b < TURN; ++b) read_b(b, IntC<0>{}, kt + 1);
     static_for<C::TN - TURN>([&](auto bc) {
       constexpr int b = TURN + decltype(bc)::value;
       static_for<C::TM>([&](auto ac) {
@@ -290,20 +289,21 @@ __device__ __forceinline__ void product_tile(const Product& q, int64_t row0, int
         }
         mul(a_, IntC<i>{});
       });
-      if constexpr (MORE) read_b(b, IntC<0>{}, kt + 1);
+      read_b(b, IntC<0>{}, kt + 1);
       __builtin_amdgcn_sched_barrier(0);
     });
   };
-  auto stage = [&](auto morec, auto fetchc, int kt, auto&& turn) {
+  // Behind the last stage it reads what happens to lie in the next slot, for nothing.
+  auto stage = [&](auto aheadc, int kt) {
     constexpr IntC<1> second{};
     constexpr IntC<-1> keep{};
     if constexpr (C::NP == 1) {
       phase(xa[0], second, kt, [&]() { read_a(xa[1], second, kt); });
-      last_phase(xa[1], morec, fetchc, kt, xa[0], turn);
+      last_phase(xa[1], aheadc, kt, xa[0]);
     } else {
       phase(xa[0], keep, kt, [&]() { read_a(xa[1], second, kt); });           // hi hi
       phase(xa[1], second, kt, []() {});                                      // lo hi
-      last_phase(xa[0], morec, fetchc, kt, xa[1], turn);                      // hi lo; lo's registers take the next hi
+      last_phase(xa[0], aheadc, kt, xa[1]);                                   // hi lo; lo's registers take the next hi
 #pragma unroll
       for (int a = 0; a < C::TM; ++a) xa[0][a] = xa[1][a];
     }
@@ -313,46 +313,36 @@ __device__ __forceinline__ void product_tile(const Product& q, int64_t row0, int
     for (int b = 0; b < C::TN; ++b) read_b(b, IntC<0>{}, kt);
     read_a(xa[0], IntC<0>{}, kt);
   };
-  if (loop > 0) {
-    if constexpr (DMA) {
+  if constexpr (HOW != THROUGH_REGISTERS) {
 #pragma unroll
-      for (int s = 0; s < C::MANY; ++s) {
-        if (s < C::NSA && s < loop) static_for<LA>([&](auto jc) { fetch_a(decltype(jc)::value, s); });
-        if (s < C::NSB && s < loop) static_for<LB>([&](auto jc) { fetch_b(decltype(jc)::value, s); });
-      }
-    } else {
-      load(0);
-      store(0);
-      if (loop > 1) load(1);
+    for (int s = 0; s < C::MANY; ++s) {
+      if (s < C::NSA) static_for<LA>([&](auto jc) { fetch_a(decltype(jc)::value, s); });
+      if (s < C::NSB) static_for<LB>([&](auto jc) { fetch_b(decltype(jc)::value, s); });
     }
-    arrive(0);
+    arrive(IntC<1>{});
     first_reads(0);
-    auto one = [&](auto morec, auto fetchc, int kt) {
-      if constexpr (!DMA) {               // the other slot: its last reader has passed the barrier of this stage
-        if (kt + 1 < loop) store(kt + 1);
-        if (kt + 2 < loop) load(kt + 2);
-      }
-      stage(morec, fetchc, kt, [&]() { arrive(kt + 1); });
-    };
-    // the stages that request both operands, the one that may request one of them, those that request nothing, the last
-    int kt = 0;
-    if constexpr (DMA) {
-      for (; kt + C::MANY < loop; ++kt) one(IntC<1>{}, IntC<2>{}, kt);
-      if (C::FEW != C::MANY && kt + C::FEW < loop) {
-        one(IntC<1>{}, IntC<1>{}, kt);
-        ++kt;
+    for (int kt = 0; kt < whole; ++kt) stage(IntC<1>{}, kt);
+    wait_lds_and<0>();                    // the loads that were for nothing write LDS too
+    if constexpr (HOW == DIRECT_AND_TAIL) {
+      if (whole < nk) {
+        __syncthreads();
+        load(whole);
+        store(whole);
+        __syncthreads();
+        first_reads(whole);
+        stage(IntC<0>{}, whole);
       }
     }
-    for (; kt + 1 < loop; ++kt) one(IntC<1>{}, IntC<0>{}, kt);
-    one(IntC<0>{}, IntC<0>{}, kt);
-  }
-  if constexpr (DMA && C::NP == 1) {
-    if (loop < nk) {                      // every wave is past its last read of the ring: the barrier of the loop's last stage
-      load(loop);
-      store(loop);
-      __syncthreads();
-      first_reads(loop);
-      stage(IntC<0>{}, IntC<0>{}, loop, []() {});
+  } else {
+    load(0);
+    store(0);
+    if (nk > 1) load(1);
+    arrive(IntC<0>{});
+    first_reads(0);
+    for (int kt = 0; kt < nk; ++kt) {
+      if (kt + 1 < nk) store(kt + 1);     // the other slot: its last reader has passed the barrier of this stage
+      if (kt + 2 < nk) load(kt + 2);
+      stage(IntC<0>{}, kt);
     }
   }
   __syncthreads();

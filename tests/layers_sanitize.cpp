@@ -65,7 +65,7 @@ int launch_norm_backward(const NormProblem& p, int dtype, const NormGrads& g, fl
 int launch_linear_forward(const LinearProblem& p, void* Y, int64_t ldy, void* Z, int64_t ldz, float*, void*) {
   ++launches;
   need(p.X && p.W && Y && p.ldx >= p.in && p.ldw >= p.in && ldy >= p.out && (!Z || ldz >= p.out) && (!p.residual || p.ldr >= p.out), "linear forward");
-  if (!linear_takes_few(p.T)) check_cut(p.T, p.out, p.in, p.dtype);
+  if (!linear_takes_few(p.T, p.out, p.in, p.dtype)) check_cut(p.T, p.out, p.in, p.dtype);
   return 0;
 }
 
