@@ -471,16 +471,16 @@ def chunkft_wgrad_adamw_fused_static(layer: Layer, begin: int, end: int, W, mast
 
 
 # ----------------------------------------------------------------- layers
-def _on_device(t, name: str, dtype):
+def _on_device(t, name: str, dtype, dev: int):
     if t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}")
     if not t.is_cuda:
         raise ValueError(f"{name} must live on the GPU")
-    if t.get_device() != _torch.cuda.current_device():
+    if t.get_device() != dev:
         raise ValueError(f"{name} must live on the current device")
 
 
-def _rows(t, name: str, width: int, dtype, rows: Optional[int] = None):
+def _rows(t, name: str, width: int, dtype, dev: int, rows: Optional[int] = None):
     """(pointer, row stride) of a 2-D device tensor of `width` columns (None: (None, 0))."""
     if t is None:
         return None, 0
@@ -489,43 +489,43 @@ def _rows(t, name: str, width: int, dtype, rows: Optional[int] = None):
         raise ValueError(f"{name} must be [{'tokens' if rows is None else rows}, {width}]")
     if s[1] != 1 and width != 1:
         raise ValueError(f"{name} must have unit inner stride")
-    _on_device(t, name, dtype)
+    _on_device(t, name, dtype, dev)
     # the stride of a dimension of one says nothing
     return t.data_ptr(), s[0] if t.shape[0] != 1 else max(s[0], width)
 
 
-def _vector(t, name: str, n: int, dtype):
+def _vector(t, name: str, n: int, dtype, dev: int):
     if t is None:
         return None
     if t.dim() != 1 or t.shape[0] != n or (t.stride(0) != 1 and n != 1):
         raise ValueError(f"{name} must be a contiguous vector of {n} elements")
-    _on_device(t, name, dtype)
+    _on_device(t, name, dtype, dev)
     return t.data_ptr()
 
 
-def _flat(t, name: str, n: int, dtype):
+def _flat(t, name: str, n: int, dtype, dev: int):
     """n elements in one piece, of whatever shape."""
     if t is None:
         return None
     if t.numel() != n or not t.is_contiguous():
         raise ValueError(f"{name} must hold {n} contiguous elements")
-    _on_device(t, name, dtype)
+    _on_device(t, name, dtype, dev)
     return t.data_ptr()
 
 
-def _grad_range(g, name: str, span: Optional[Tuple[int, int]], n: int):
+def _grad_range(g, name: str, span: Optional[Tuple[int, int]], n: int, dev: int):
     """(pointer, begin, end) of the fp32 gradient of the elements [begin, end) of a vector (None: all of them)."""
     if g is None:
         return None, 0, 0
     begin, end = (0, n) if span is None else span
-    return _vector(g, name, end - begin, _torch.float32), begin, end
+    return _vector(g, name, end - begin, _torch.float32, dev), begin, end
 
 
-def _workspace(ws):
+def _workspace(ws, dev: int):
     if ws is None:
         return None, 0
     n = ws.numel()
-    return _flat(ws, "ws", n, ws.dtype), n * ws.element_size()
+    return _flat(ws, "ws", n, ws.dtype, dev), n * ws.element_size()
 
 
 def _dtype_of(layer):
@@ -537,9 +537,9 @@ def make_norm(kind: int, X, w=None, b=None, eps: float = 1e-5) -> NormLayer:
     d = _torch_dtype_code(X)
     if X.dim() != 2:
         raise ValueError("X must be 2-D")
-    n = X.shape[1]
-    p, ld = _rows(X, "X", n, X.dtype)
-    layer = NormLayer(kind, d, X.shape[0], n, p, ld, _vector(w, "w", n, X.dtype), _vector(b, "b", n, X.dtype), float(eps))
+    n, dt, dev = X.shape[1], X.dtype, _torch.cuda.current_device()
+    p, ld = _rows(X, "X", n, dt, dev)
+    layer = NormLayer(kind, d, X.shape[0], n, p, ld, _vector(w, "w", n, dt, dev), _vector(b, "b", n, dt, dev), float(eps))
     layer.tensors = X, w, b                                 # alive as long as the description is
     return layer
 
@@ -550,30 +550,31 @@ def chunkft_norm_workspace_bytes(layer: NormLayer) -> int:
 
 def chunkft_norm_forward(layer: NormLayer, Y, stats=None, stream=None, check: bool = True) -> int:
     """stats: None or a contiguous fp32 [tokens, 2] tensor (mean and reciprocal deviation of every token)."""
-    p, ld = _rows(Y, "Y", layer.n, _dtype_of(layer), layer.T)
-    st = lib().chunkft_norm_forward(C.byref(layer), p, ld, _stats(stats, layer), _stream_ptr(stream))
+    dev = _torch.cuda.current_device()
+    p, ld = _rows(Y, "Y", layer.n, _dtype_of(layer), dev, layer.T)
+    st = lib().chunkft_norm_forward(C.byref(layer), p, ld, _stats(stats, layer, dev), _stream_ptr(stream))
     if check and st != OK:
         raise ChunkFTError(st, "chunkft_norm_forward")
     return st
 
 
-def _stats(stats, layer: NormLayer):
+def _stats(stats, layer: NormLayer, dev: int):
     if stats is None:
         return None
     if tuple(stats.shape) != (layer.T, 2):
         raise ValueError("stats must be [tokens, 2]")
-    return _flat(stats, "stats", 2 * layer.T, _torch.float32)
+    return _flat(stats, "stats", 2 * layer.T, _torch.float32, dev)
 
 
 def chunkft_norm_backward(layer: NormLayer, stats, dY, dX=None, dw=None, w_range=None, db=None, b_range=None,
                           accumulate: bool = False, ws=None, stream=None, check: bool = True) -> int:
     """w_range, b_range: (begin, end) of the elements that dw and db hold (None: all)."""
-    T, dt = layer.T, _dtype_of(layer)
-    py, ldy = _rows(dY, "dY", layer.n, dt, T)
-    px, ldx = _rows(dX, "dX", layer.n, dt, T)
-    pw, pb = _grad_range(dw, "dw", w_range, layer.n), _grad_range(db, "db", b_range, layer.n)
-    st = lib().chunkft_norm_backward(C.byref(layer), _stats(stats, layer), py, ldy, px, ldx, *pw, *pb, int(accumulate),
-                                     *_workspace(ws), _stream_ptr(stream))
+    T, dt, dev = layer.T, _dtype_of(layer), _torch.cuda.current_device()
+    py, ldy = _rows(dY, "dY", layer.n, dt, dev, T)
+    px, ldx = _rows(dX, "dX", layer.n, dt, dev, T)
+    pw, pb = _grad_range(dw, "dw", w_range, layer.n, dev), _grad_range(db, "db", b_range, layer.n, dev)
+    st = lib().chunkft_norm_backward(C.byref(layer), _stats(stats, layer, dev), py, ldy, px, ldx, *pw, *pb, int(accumulate),
+                                     *_workspace(ws, dev), _stream_ptr(stream))
     if check and st != OK:
         raise ChunkFTError(st, "chunkft_norm_backward")
     return st
@@ -584,14 +585,14 @@ def make_linear(X, W, bias=None, activation: int = ACT_NONE, residual=None, toke
     d = _torch_dtype_code(W)
     if W.dim() != 2:
         raise ValueError("W must be 2-D")
-    out, n_in = W.shape
-    pw, ldw = _rows(W, "W", n_in, W.dtype)
-    px, ldx = _rows(X, "X", n_in, W.dtype, tokens)
+    (out, n_in), dt, dev = W.shape, W.dtype, _torch.cuda.current_device()
+    pw, ldw = _rows(W, "W", n_in, dt, dev)
+    px, ldx = _rows(X, "X", n_in, dt, dev, tokens)
     T = X.shape[0] if X is not None else tokens
     if T is None:
         raise ValueError("give X or tokens")
-    pr, ldr = _rows(residual, "residual", out, W.dtype, T)
-    layer = LinearLayer(d, activation, out, n_in, T, px, ldx, pw, ldw, _vector(bias, "bias", out, W.dtype), pr, ldr)
+    pr, ldr = _rows(residual, "residual", out, dt, dev, T)
+    layer = LinearLayer(d, activation, out, n_in, T, px, ldx, pw, ldw, _vector(bias, "bias", out, dt, dev), pr, ldr)
     layer.tensors = X, W, bias, residual                    # alive as long as the description is
     return layer
 
@@ -601,9 +602,9 @@ def chunkft_linear_workspace_bytes(layer: LinearLayer, backward: bool = False) -
 
 
 def chunkft_linear_forward(layer: LinearLayer, Y, Z=None, ws=None, stream=None, check: bool = True) -> int:
-    dt = _dtype_of(layer)
-    st = lib().chunkft_linear_forward(C.byref(layer), *_rows(Y, "Y", layer.out, dt, layer.T), *_rows(Z, "Z", layer.out, dt, layer.T),
-                                      *_workspace(ws), _stream_ptr(stream))
+    dt, dev = _dtype_of(layer), _torch.cuda.current_device()
+    st = lib().chunkft_linear_forward(C.byref(layer), *_rows(Y, "Y", layer.out, dt, dev, layer.T), *_rows(Z, "Z", layer.out, dt, dev, layer.T),
+                                      *_workspace(ws, dev), _stream_ptr(stream))
     if check and st != OK:
         raise ChunkFTError(st, "chunkft_linear_forward")
     return st
@@ -612,12 +613,12 @@ def chunkft_linear_forward(layer: LinearLayer, Y, Z=None, ws=None, stream=None, 
 def chunkft_linear_backward(layer: LinearLayer, dY, Z=None, dZ=None, dX=None, db=None, b_range=None, accumulate: bool = False,
                             ws=None, stream=None, check: bool = True) -> int:
     """Without an activation Z and dZ are ignored (dz is dY).  b_range: (begin, end) of the elements that db holds (None: all)."""
-    dt, T = _dtype_of(layer), layer.T
+    dt, T, dev = _dtype_of(layer), layer.T, _torch.cuda.current_device()
     if layer.activation == ACT_NONE:
         Z = dZ = None
-    st = lib().chunkft_linear_backward(C.byref(layer), *_rows(dY, "dY", layer.out, dt, T), *_rows(Z, "Z", layer.out, dt, T),
-                                       *_rows(dZ, "dZ", layer.out, dt, T), *_rows(dX, "dX", layer.n_in, dt, T),
-                                       *_grad_range(db, "db", b_range, layer.out), int(accumulate), *_workspace(ws),
+    st = lib().chunkft_linear_backward(C.byref(layer), *_rows(dY, "dY", layer.out, dt, dev, T), *_rows(Z, "Z", layer.out, dt, dev, T),
+                                       *_rows(dZ, "dZ", layer.out, dt, dev, T), *_rows(dX, "dX", layer.n_in, dt, dev, T),
+                                       *_grad_range(db, "db", b_range, layer.out, dev), int(accumulate), *_workspace(ws, dev),
                                        _stream_ptr(stream))
     if check and st != OK:
         raise ChunkFTError(st, "chunkft_linear_backward")
@@ -634,10 +635,10 @@ def chunkft_orthogonalize(G, O, steps: int = 5, eps: float = 1e-7, ws=None, stre
     d = _torch_dtype_code(G)
     if G.dim() != 2:
         raise ValueError("G must be 2-D")
-    rows, cols = G.shape
-    pg, ldg = _rows(G, "G", cols, G.dtype)
-    po, ldo = _rows(O, "O", cols, G.dtype, rows)
-    st = lib().chunkft_orthogonalize(pg, ldg, d, rows, cols, steps, eps, po, ldo, *_workspace(ws), _stream_ptr(stream))
+    (rows, cols), dt, dev = G.shape, G.dtype, _torch.cuda.current_device()
+    pg, ldg = _rows(G, "G", cols, dt, dev)
+    po, ldo = _rows(O, "O", cols, dt, dev, rows)
+    st = lib().chunkft_orthogonalize(pg, ldg, d, rows, cols, steps, eps, po, ldo, *_workspace(ws, dev), _stream_ptr(stream))
     if check and st != OK:
         raise ChunkFTError(st, "chunkft_orthogonalize")
     return st
@@ -653,9 +654,10 @@ def chunkft_muon_chunk(g, master, m, W_at_begin, rows: int, cols: int, hp: MuonH
     """The update of `rows` whole rows of `cols` columns; g, master, m hold rows * cols floats, W_at_begin (or None) the segment's
     rows * cols elements of the parameter."""
     torch, n = _torch_module(), rows * cols
-    W = _flat(W_at_begin, "W_at_begin", n, torch.float32 if w_dtype == F32 else torch.bfloat16)
-    st = lib().chunkft_muon_chunk(*[_flat(t, name, n, torch.float32) for t, name in ((g, "g"), (master, "master"), (m, "m"))], W, w_dtype,
-                                  rows, cols, C.byref(hp), *_workspace(ws), _stream_ptr(stream))
+    dev = torch.cuda.current_device()
+    W = _flat(W_at_begin, "W_at_begin", n, torch.float32 if w_dtype == F32 else torch.bfloat16, dev)
+    st = lib().chunkft_muon_chunk(*[_flat(t, name, n, torch.float32, dev) for t, name in ((g, "g"), (master, "master"), (m, "m"))], W, w_dtype,
+                                  rows, cols, C.byref(hp), *_workspace(ws, dev), _stream_ptr(stream))
     if check and st != OK:
         raise ChunkFTError(st, "chunkft_muon_chunk")
     return st
