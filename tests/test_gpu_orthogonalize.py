@@ -155,3 +155,18 @@ def test_muon_chunk_without_weights_with_fp32_weights_and_in_a_graph():
         B.chunkft_orthogonalize(g, torch.empty_like(g), ws=ws)
     torch.cuda.synchronize()
     assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1]) and torch.equal(a[2], a[0])
+
+
+@pytest.mark.parametrize("rows,cols", [(512, 512), (300, 1100), (1100, 300)])
+def test_three_steps_from_small_singular_values_keep_float32(rows, cols):
+    """Every singular value is small, so each step is nearly x -> a x and keeps relative errors as they are.  A step adds at most
+    2^-22 / 3 from the two parts (each residue is uniform: its root mean square is its largest value over sqrt 3), 2^-24 / sqrt 3 each
+    from the product a x and the sum, and four roundings of 2^-24 of factors common to all values: 3.8e-7.  The last step's products
+    add sqrt(3 K / 32) roundings of 2^-24 of a part smaller than a x: 4.4e-7 for K = 512.  Three steps: 1.6e-6."""
+    g = torch.randn(rows, cols, generator=torch.Generator().manual_seed(rows))
+    o = torch.empty(rows, cols, device=DEV)
+    B.chunkft_orthogonalize(g.to(DEV), o, steps=3, eps=0.0, ws=_ws(B.F32, rows, cols))
+    torch.cuda.synchronize()
+    want = newton_schulz64(g.double(), 3, 0.0)
+    err = float(torch.linalg.matrix_norm(o.cpu().double() - want) / torch.linalg.matrix_norm(want))
+    assert err <= 1.6e-6, err
