@@ -16,6 +16,7 @@
  * identical inputs giving identical bits, no exceptions.  Inputs and outputs of a call do not overlap unless it says so.
  * A workspace is scratch: calls that may overlap in time need workspaces of their own (so do graphs that may).
  * Types: CHUNKFT_BF16 or CHUNKFT_F32; every sum, statistic and state is fp32 (or wider), a result is rounded once, to nearest.
+ * A call whose launch would need 2^32 lanes or more is refused with ERR_HIP.
  * Any alignment of the element type is accepted; rows of 16 bytes at 16-byte addresses are fastest.
  */
 #ifndef CHUNKFT_LAYERS_API_H

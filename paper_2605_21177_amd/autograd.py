@@ -100,8 +100,6 @@ def _weight_gradient(seg: ChunkSegment, X, dY, W) -> None:
     out, n_in = W.shape
     layer = B.make_layer(B.LINEAR, X, dY, out, n_in, split_k=seg.split_k)
     muon = seg.fused and isinstance(seg.hp, B.MuonHparams)
-    if muon and (seg.begin % n_in or seg.end % n_in):
-        raise ValueError("the orthogonalised update takes whole rows")
     first = seg.micro_batches == 0
     seg.one_more()
     ws = seg.workspace(layer)
@@ -246,9 +244,10 @@ class _NormLayer(torch.autograd.Function):
 
 
 def _as_rows(t, width: int):
-    """t as [tokens, width] with unit inner stride."""
+    """t as [tokens, width] with unit inner stride and rows that do not overlap (an expanded tensor's do)."""
     t2 = t if t.dim() == 2 else t.reshape(-1, width)
-    return t2 if t2.stride(1) == 1 or width == 1 else t2.contiguous()
+    row, element = t2.stride()
+    return t2 if element == 1 and row >= width else t2.clone(memory_format=torch.contiguous_format)
 
 
 def _open(segs) -> None:
@@ -282,6 +281,11 @@ def _inside(seg: Optional[ChunkSegment], n: int) -> None:
         raise ValueError("the segment must lie in the vector, and a vector has no orthogonalised update")
 
 
+def _apart(a: Optional[ChunkSegment], b: Optional[ChunkSegment]) -> None:
+    if a is not None and a is b and a.active:
+        raise ValueError("each tensor needs a segment of its own")
+
+
 def _anchor_for(x, *segs):
     """A leaf of this call alone that makes autograd run backward where only a segment wants it."""
     if x.requires_grad or not torch.is_grad_enabled() or not any(s is not None and s.active for s in segs):
@@ -306,6 +310,8 @@ def chunk_linear(x: torch.Tensor, W: torch.Tensor, seg: Optional[ChunkSegment], 
         raise ValueError("W must be contiguous (the chunk is a range of its flattened elements)")
     if bias is None and bias_seg is not None:
         raise ValueError("a segment of a bias needs the bias")
+    if seg is not None and seg.active and isinstance(seg.hp, B.MuonHparams) and (seg.begin % W.shape[1] or seg.end % W.shape[1]):
+        raise ValueError("the orthogonalised update takes whole rows")
     if bias is not None or activation != B.ACT_NONE or residual is not None:
         out, n_in = W.shape
         if x.shape[-1] != n_in or x.dtype is not W.dtype:
@@ -313,6 +319,9 @@ def chunk_linear(x: torch.Tensor, W: torch.Tensor, seg: Optional[ChunkSegment], 
         if bias is not None:
             _frozen(bias, "bias", out, W.dtype)
         _inside(bias_seg, out)
+        _apart(seg, bias_seg)
+        if seg is not None and seg.active and seg.end > W.numel():
+            raise ValueError("the segment must lie in W")
         if residual is not None and (residual.shape != x.shape[:-1] + (out,) or residual.dtype is not W.dtype):
             raise ValueError("residual must have the output's shape and type")
         anchor = _anchor_for(x, seg, bias_seg)
@@ -338,6 +347,7 @@ def chunk_norm(x: torch.Tensor, w: Optional[torch.Tensor], b: Optional[torch.Ten
         elif vec_seg is not None:
             raise ValueError(f"a segment of {name} needs {name}")
         _inside(vec_seg, n)
+    _apart(seg, bias_seg)
     anchor = _anchor_for(x, seg, bias_seg)
     keep = anchor is not None or (x.requires_grad and torch.is_grad_enabled())
     return _NormLayer.apply(x, w, b, anchor, kind, eps, seg, bias_seg, keep)

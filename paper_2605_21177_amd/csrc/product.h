@@ -120,8 +120,8 @@ struct Fetcher {
   __device__ __forceinline__ void load(int64_t kt, int wave, int lane, u32x4_t (&v)[LOADS]) const {
     const unsigned short* b = base;
     // Away from the end of k nothing has to be looked at: rows (pieces) that are not there repeat the first one, and a piece that a
-    // row across k ends in runs on into the next row, for columns that are not stored.
-    if (KS ? (kt + 1) * BK < K : (kt + 1) * BK <= K) {
+    // row across k ends in runs on into the next rows (up to seven, of one element each), for columns that are not stored.
+    if (KS ? (kt + 1) * BK + 7 <= K : (kt + 1) * BK <= K) {
       b += KS ? kt * BK * ld : kt * BK;
 #pragma unroll
       for (int i = 0; i < LOADS; ++i) {

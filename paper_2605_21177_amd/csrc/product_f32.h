@@ -39,8 +39,8 @@ __device__ __forceinline__ void product_tile_f32(const ProductF32& q, int64_t ro
   Row<float> va[C::LA], vb[C::LB];
   auto load = [&](int64_t kt) {
     // Away from the end of k nothing has to be looked at: rows (pieces) that are not there repeat the first one, and a piece that a
-    // row across k ends in runs on into the next row, for columns that are not stored.
-    if (KB ? (kt + 1) * C::BK < q.K : (kt + 1) * C::BK <= q.K) {
+    // row across k ends in runs on into the next rows (up to three, of one element each), for columns that are not stored.
+    if (KB ? (kt + 1) * C::BK + 3 <= q.K : (kt + 1) * C::BK <= q.K) {
       const float* const a = q.A + row0 * q.lda + kt * C::BK;
       const float* const b = KB ? q.B + kt * C::BK * q.ldb + col0 : q.B + col0 * q.ldb + kt * C::BK;
 #pragma unroll

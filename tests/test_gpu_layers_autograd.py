@@ -239,3 +239,26 @@ def test_captured_step_beside_a_living_eager_graph():
         for k in SHAPES:
             assert torch.equal(captured[k].g, segs[k].g), k
         x.mul_(0.5)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_expanded_gradients_inputs_and_residuals(dtype):
+    """Rows that share their memory: the gradient behind a sum over the tokens, an input and a residual that are one row repeated,
+    and a layer of one output, whose gradient behind a sum is one number repeated."""
+    p = _params(18, dtype)
+    dev = {k: v.to(DEV) for k, v in p.items()}
+    x, R = _data(19, dtype, (1, 1))
+    row, R = x[0], R[0, 0]
+    xd = row.to(DEV).requires_grad_()
+    y = _block(xd.expand(9, D), dev, {})
+    (y.sum(0) * R.to(DEV)).sum().backward()
+    ref_y, ref_dx, _ = _grads64(row, 9 * R, p)
+    assert y.shape == (9, D) and _off(y[3], ref_y) <= BOUND[dtype]
+    assert _off(xd.grad, ref_dx) <= 2 * BOUND[dtype]                       # nine equal rows summed in the type: eight roundings more
+    W, b = dev["W1"][:1].contiguous(), dev["b1"][:1].contiguous()
+    seg, bias_seg = (A.ChunkSegment(0, n, torch.empty(n, device=DEV)) for n in (D, 1))
+    xs = torch.randn(40, D, generator=torch.Generator().manual_seed(20)).to(dtype)
+    xd = xs.to(DEV).requires_grad_()
+    A.chunk_linear(xd, W, seg, bias=b, bias_seg=bias_seg).sum().backward()
+    assert torch.equal(xd.grad, W.expand(40, D)) and float(bias_seg.g) == 40.0
+    assert _off(seg.g, xs.double().sum(0)) <= BOUND[dtype]

@@ -195,3 +195,20 @@ def test_same_bits_again_and_in_a_graph_on_another_stream():
         d["x"].mul_(1.5)
         step(eager)
         torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("dtype", sorted(DTYPES))
+@pytest.mark.parametrize("n_in", [1, 2, 3])
+@pytest.mark.parametrize("out", [65, 66, 71, 128, 135])
+def test_input_gradient_of_rows_narrower_than_a_piece(n_in, out, dtype):
+    """16 bytes of W hold several of its rows; what lies behind the last one is not a number."""
+    dt, T = DTYPES[dtype], 40
+    d = _inputs(n_in * 100 + out, T, n_in, out, dt)
+    room = torch.full((out * n_in + 64,), float("nan"), dtype=dt, device=DEV)
+    room[:out * n_in] = d["W"].reshape(-1).to(DEV)
+    dx = torch.empty(T, n_in, dtype=dt, device=DEV)
+    layer = B.make_linear(None, room[:out * n_in].view(out, n_in), tokens=T)
+    B.chunkft_linear_backward(layer, d["dy"].to(DEV), dX=dx, ws=_ws(layer, True))
+    torch.cuda.synchronize()
+    W, dy = d["W"].double(), d["dy"].double()
+    assert_close(dx, dy @ W, (out + 4) * (dy.abs() @ W.abs()), 1, "dx")

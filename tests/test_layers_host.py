@@ -235,3 +235,17 @@ def test_host_code_of_the_layers_under_sanitizers(tmp_path):
     assert r.returncode == 0, r.stderr[-2000:]
     r = subprocess.run([exe], capture_output=True, text=True, timeout=300)
     assert r.returncode == 0 and r.stdout.startswith("ok:"), (r.stdout[-1000:], r.stderr[-3000:])
+
+
+def test_segments_that_no_call_can_serve():
+    x, W, b, w = torch.zeros(3, 8), torch.zeros(8, 8), torch.zeros(8), torch.zeros(8)
+    seg, t = A.ChunkSegment(0, 8, torch.zeros(8)), torch.zeros(8)
+    with pytest.raises(ValueError, match="of its own"):
+        A.chunk_linear(x, W, seg, bias=b, bias_seg=seg)
+    with pytest.raises(ValueError, match="of its own"):
+        A.chunk_norm(x, w, b, B.LAYERNORM, seg=seg, bias_seg=seg)
+    with pytest.raises(ValueError, match="lie in W"):
+        A.chunk_linear(x, W, A.ChunkSegment(60, 65, torch.zeros(5)), activation=B.ACT_RELU)
+    for activation in (B.ACT_NONE, B.ACT_RELU):
+        with pytest.raises(ValueError, match="whole rows"):
+            A.chunk_linear(x, W, A.ChunkSegment(4, 12, master=t, m=t, hp=B.muon_hparams(0.1)), activation=activation)
