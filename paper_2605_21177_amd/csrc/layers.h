@@ -79,7 +79,7 @@ constexpr int kGateLanes = 32, kGateRows = 8;       // of the pass over dy and z
 // Rows of partial sums (of norm_pitch(out) floats) that a backward pass leaves for the bias.
 int64_t linear_parts(int64_t T, int64_t out, int dtype, int compute_units);
 
-// How a product [M, K] x [K, N] is cut: square tiles of `tile`, `slabs` runs of kslab values of k.  From the shape alone: the workspace
+// How a product [M, K] x [K, N] is cut: square tiles of `tile` (bf16: 64 is 64 x 128), `slabs` runs of kslab values of k.  From the shape alone: the workspace
 // that the caller gives depends on it.
 struct LinearPlan {
   int32_t tile, slabs;

@@ -13,10 +13,11 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // What a cut costs, in us, from rounds of workgroups (n items of a tile with ks values of k each on so many compute units) and the
 // slabs' traffic.  Measured per 1024 k (and 1 - 2 us around them): bf16, 256-wide tiles, one to a unit, 19.5 where few units have
-// one and 24 where all have; 128-wide ones 10.2 alone on a unit, 14.5 the pair.  fp32: 22 and 18.2 for 64-wide ones alone and
+// one and 24 where all have; 128-wide ones 10.2 alone on a unit, 14.5 the pair; 64 x 128 ones 7.5 alone, 10 the pair.  fp32: 22 and 18.2 for 64-wide ones alone and
 // each of several, 72 and 64.5 for 128-wide ones.  Slabs: 8 bytes per slab and element at 7 TB/s, and a launch.
 // E.g. bf16, 4096 x 4096 x 14336: 256-wide tiles 388 us, 128-wide 419; 512 x 14336 x 4096 one slab of 128-wide tiles 146, four 64;
-// 1024 x 14336 x 4096 162 and, four slabs of 256-wide tiles, 108.
+// 1024 x 14336 x 4096 162 and, four slabs of 256-wide tiles, 108; 1024 x 2048 x 2048 128-wide tiles 24.3, 64 x 128 ones 15.9 (one to a
+// unit where half of them had none), 2048 x 2048 x 2048 26.4 and 24.5, 4096 x 2048 x 2048 34 and 50.
 double round_cost(int dtype, int tile, double items, double ks, double units) {
   const double k = ks / 1024;
   if (dtype == 0) {
@@ -28,7 +29,8 @@ double round_cost(int dtype, int tile, double items, double ks, double units) {
     return full * (24 * k + 2) + (rest > 0 ? (19.5 + 4.5 * rest) * k + 2 : 0);
   }
   const double full = std::floor(items / (2 * units)), rest = items - full * 2 * units;
-  return full * (14.5 * k + 1) + (rest > units ? 14.5 * k + 1 : rest > 0 ? 10.2 * k + 1 : 0);
+  const double alone = tile == 64 ? 7.5 : 10.2, pair = tile == 64 ? 10 : 14.5;
+  return full * (pair * k + 1) + (rest > units ? pair * k + 1 : rest > 0 ? alone * k + 1 : 0);
 }
 
 // Time in us of `n` workgroups of a tile with ks values of k each.  Measured per 1024 k, one part / two: 128-wide tiles 10.2 / 19.5
@@ -88,14 +90,14 @@ int64_t linear_parts(int64_t T, int64_t out, int dtype, int compute_units) {
 }
 
 LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, int dtype, int compute_units) {
-  const int small = dtype == 0 ? 64 : 128;
   const int64_t unit = dtype == 0 ? 32 : 64;                 // k of a stage: slabs are whole stages
-  // rows without 16-byte pieces go through registers, in small tiles (fp32 always does)
+  // rows without 16-byte pieces go through registers, in 128-wide tiles (fp32 always does, in 64- and 128-wide ones)
   const bool direct = K % 8 == 0 && N % 8 == 0;
-  LinearPlan best{small, 1, K};
+  const int first = dtype == 0 || direct ? 64 : 128, last = dtype != 0 && direct ? 256 : 128;
+  LinearPlan best{first, 1, K};
   double least = -1;
-  for (int tile = small; tile <= (direct || dtype == 0 ? 2 * small : small); tile *= 2) {
-    const double tiles = (double)ceil_div(M, tile) * (double)ceil_div(N, tile);
+  for (int tile = first; tile <= last; tile *= 2) {
+    const double tiles = (double)ceil_div(M, tile) * (double)ceil_div(N, dtype != 0 && tile == 64 ? 128 : tile);
     for (int want = 1; want <= 16; ++want) {
       const int64_t ks = ceil_div(ceil_div(K, want), unit) * unit;
       const int64_t slabs = ceil_div(K, ks);

@@ -321,6 +321,7 @@ typedef ProductCfg<256, 256, 4, 2, 3, 2> Tile256;
 // GELU and z 131 us and 122, 4096 x 4096 x 14336 455 and 440; 4096 x 14336 x 4096, as much x as W, 362 and 370.
 typedef ProductCfg<256, 256, 4, 2, 2, 3> Tile256W;
 typedef ProductCfg<128, 128, 2, 2, 2, 2> Tile128;
+typedef ProductCfg<64, 128, 2, 2, 2, 2> Tile64;      // where 128-wide tiles leave units without one
 
 template <class C, int KB, int HOW, bool SPLIT>
 int launch_tiles(const Product& q, const Epilogue& e, const Slabs& s, hipStream_t st) {
@@ -370,7 +371,8 @@ int launch_product(const void* A, int64_t lda, const void* B, int64_t ldb, int64
     if (!direct) return launch_tiles<Tile128, KB, THROUGH_REGISTERS, S>(q, e, s, st);
     auto by_tail = [&](auto how) {
       constexpr int HOW = decltype(how)::value;
-      if (plan.tile != 256) return launch_tiles<Tile128, KB, HOW, S>(q, e, s, st);
+      if (plan.tile == 64) return launch_tiles<Tile64, KB, HOW, S>(q, e, s, st);
+      if (plan.tile == 128) return launch_tiles<Tile128, KB, HOW, S>(q, e, s, st);
       if constexpr (!KB) {
         if (N > M) return launch_tiles<Tile256W, KB, HOW, S>(q, e, s, st);
       }
