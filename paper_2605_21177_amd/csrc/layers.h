@@ -129,7 +129,7 @@ inline int64_t ns_half_tiles(int64_t r, int tile) {
 constexpr int kNsNormBlocks = 1024;      // most partial sums of the norm
 struct NsLayout {
   int64_t rows_p, cols_p, r;             // padded to whole stages of k; the padded small side
-  size_t x, a, sums, total;              // bytes of a buffer of X, of A, of the slabs' sums, of all
+  size_t x, a, diag, sums, total;        // bytes of a buffer of X, of A, of a diagonal, of the slabs' sums, of all
 };
 NsLayout ns_layout(int64_t rows, int64_t cols, int parts, int compute_units);
 

@@ -162,13 +162,14 @@ NsLayout ns_layout(int64_t rows, int64_t cols, int parts, int compute_units) {
   const int64_t c = l.rows_p < l.cols_p ? l.cols_p : l.rows_p;
   l.x = (size_t)l.rows_p * (size_t)l.cols_p * 2u * (size_t)parts;
   l.a = (size_t)l.r * (size_t)l.r * 2u * (size_t)parts;
+  l.diag = (size_t)l.r * 4u;
   l.sums = 0;
   for (int64_t k : {c, l.r}) {
     const NsCut cut = ns_cut(l.r, k, parts, compute_units);
     const size_t need = cut.slabs > 1 ? (size_t)cut.slabs * (size_t)ns_half_tiles(l.r, cut.tile) * (size_t)(cut.tile * cut.tile) * 4u : 0;
     if (need > l.sums) l.sums = need;
   }
-  l.total = 256 + kNsNormBlocks * sizeof(double) + 2 * l.x + 2 * l.a + l.sums;
+  l.total = 256 + kNsNormBlocks * sizeof(double) + 2 * l.x + 2 * l.a + l.diag + l.sums;
   return l;
 }
 

@@ -26,6 +26,7 @@ struct NsBuffers {
   unsigned short* x1;
   unsigned short* a;
   unsigned short* poly;
+  float* diag;                     // of a I + b A + c A^2; the polynomial itself is held without it
   float* sums;                     // slabs of A's and the polynomial's tiles
 };
 template <int NP> int run_newton_schulz(const OrthoProblem& p, const NsBuffers& b, hipStream_t st);

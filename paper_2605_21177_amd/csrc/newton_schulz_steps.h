@@ -15,6 +15,7 @@ struct StepArgs {
   TileOrder order;               // APPLY, LAST
   int n_items;
   const NsScalars* sc;           // nullptr after the first step
+  float* diag;                   // written by POLY, read by APPLY and LAST
   const unsigned short* X;       // APPLY, LAST: what the step starts from
   int64_t ldx;
   unsigned short* D;             // what the step writes
@@ -51,12 +52,6 @@ __device__ __forceinline__ void put_result(T* p, int64_t valid, const float (&v)
   }
 }
 
-// Where a X is added: to the products' sums in fp32, or inside them, with a I in the polynomial.  Inside, each sum carries a X
-// through all its additions and the polynomial's diagonal is rounded to its digits: fp32 results are off by 6e-6 after three steps
-// on 2048 x 2048 instead of 1.5e-7, and adding it apart costs them 3%.  Results of 8 digits lose nothing by it (1.92e-3 and 1.95e-3
-// apart after five steps) and save the second reading of X: 1340 us, not 1380, at 4096 x 4096.
-template <int NP> constexpr bool kAddsApart = NP == 2;
-
 // Factor that turns a step's sums into values.
 template <int STEP>
 __device__ __forceinline__ float step_factor(const StepArgs& s) {
@@ -73,25 +68,36 @@ __device__ __forceinline__ void finish_half(const StepArgs& s, float f, int64_t 
     float a[8];
     load_parts<NP>(s.q.A + r * s.q.lda + stored<NP>(c), a);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = fmaf(kNsC, v[e], kNsB * (a[e] * (1.f / kScaleA))) + (!kAddsApart<NP> && r == c + e ? kNsA : 0.f);
+    for (int e = 0; e < 8; ++e) v[e] = fmaf(kNsC, v[e], kNsB * (a[e] * (1.f / kScaleA)));
+    if (r >= c && r < c + 8) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if (r != c + e) continue;
+        s.diag[r] = v[e] + kNsA;
+        v[e] = 0.f;
+      }
+    }
   }
 #pragma unroll
   for (int e = 0; e < 8; ++e) v[e] *= STEP == GRAM ? kScaleA : kScaleP;
 }
 
-// Eight values of (a I + b A + c A^2) X at row r and column c, from their sums.
-template <int NP>
+// Eight values of (a I + b A + c A^2) X (BY_ROW), or of X times it, at row r and column c, from the sums without the diagonal's part.
+template <int NP, bool BY_ROW>
 __device__ __forceinline__ void finish_apply(const StepArgs& s, float f, int64_t r, int64_t c, float (&v)[8]) {
-  if constexpr (!kAddsApart<NP>) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] *= f;
-    return;
-  }
-  float x[8];
+  float x[8], d[8];
   load_parts<NP>(s.X + r * s.ldx + stored<NP>(c), x);
-  const float a = kNsA * (f * kScaleP);
+  if constexpr (BY_ROW) {
+    const float of_row = s.diag[r];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] = fmaf(f, v[e], a * x[e]);
+    for (int e = 0; e < 8; ++e) d[e] = of_row;
+  } else {
+    *(f32x4*)d = *(const f32x4*)(s.diag + c);
+    *(f32x4*)(d + 4) = *(const f32x4*)(s.diag + c + 4);
+  }
+  const float down = f * kScaleP;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = fmaf(f, v[e], d[e] * (down * x[e]));
 }
 
 template <class C, int STEP, int KA, int KB, bool SPLIT>
@@ -127,14 +133,14 @@ __global__ __launch_bounds__(C::NT, 2) void step_kernel(const StepArgs s) {
       store_parts<NP>(s.D + r * s.ldd + stored<NP>(c), v);
     } else if constexpr (STEP == APPLY) {
       if (r >= q.M || c >= q.N) return;
-      finish_apply<NP>(s, f, r, c, v);
+      finish_apply<NP, KB != 0>(s, f, r, c, v);
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] *= kScaleX;
       store_parts<NP>(s.D + r * s.ldd + stored<NP>(c), v);
     } else {
       if (r >= s.rows || c >= s.cols) return;
       const int64_t valid = s.cols - c;
-      finish_apply<NP>(s, f, r, c, v);
+      finish_apply<NP, KB != 0>(s, f, r, c, v);
       if (!s.master) {
         if (s.o_dtype == 0) put_result((float*)s.O + r * s.ldo + c, valid, v);
         else put_result((unsigned short*)s.O + r * s.ldo + c, valid, v);
@@ -257,6 +263,7 @@ int run_newton_schulz(const OrthoProblem& p, const NsBuffers& b, hipStream_t st)
   for (int k = 0; k < p.steps && err == 0; ++k) {
     StepArgs s{};
     s.sc = k == 0 ? b.sc : nullptr;
+    s.diag = b.diag;
     s.D = b.a;
     s.ldd = lda;
     s.q = Product{x0, x0, ldx, ldx, b.r, b.r, tall ? b.rows_p : b.cols_p};
