@@ -84,8 +84,16 @@ int64_t linear_parts(int64_t T, int64_t out, int dtype, int compute_units);
 struct LinearPlan {
   int32_t tile, slabs;
   int64_t kslab;
+  bool pack;            // operands are copied to rows of whole 128-byte lines, first, where they are not so already
 };
 LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, int dtype, int compute_units);
+// Rows and elements of a row of a packed operand (whole stages of k, whole lines), and bytes of a plan's parts of the workspace, in this
+// order: the slabs' sums, A [M, K], B ([N, K], or [K, N] across).
+inline int64_t packed_pitch(int64_t n) { return (n + 63) / 64 * 64; }
+struct LinearSpace {
+  size_t slabs, a, b;
+};
+LinearSpace linear_space(const LinearPlan& plan, int64_t M, int64_t N, int64_t K, bool across);
 bool linear_takes_few(int64_t T, int64_t out, int64_t in, int dtype);   // the forward pass is one pass over the weights, whatever the plan
 
 int launch_linear_forward(const LinearProblem& p, void* Y, int64_t ldy, void* Z, int64_t ldz, float* ws, void* stream);

@@ -68,19 +68,19 @@ int check_linear(const chunkft_linear* L, LinearProblem* p) {
   return CHUNKFT_OK;
 }
 
-// Sums of slabs of a product, rows of `N` padded columns.
-size_t slab_need(int64_t M, int64_t N, int64_t K, int32_t dtype) {
-  const LinearPlan plan = linear_plan(M, N, K, dtype, device_compute_units());
-  return plan.slabs <= 1 ? 0 : static_cast<size_t>(plan.slabs) * static_cast<size_t>(M) * static_cast<size_t>(norm_pitch(N)) * 4u;
+// A product's slabs and packed operands.
+size_t product_need(int64_t M, int64_t N, int64_t K, int32_t dtype, bool across) {
+  const LinearSpace l = linear_space(linear_plan(M, N, K, dtype, device_compute_units()), M, N, K, across);
+  return l.slabs + l.a + l.b;
 }
 
-size_t forward_need(const LinearProblem& p) { return linear_takes_few(p.T, p.out, p.in, p.dtype) ? 0 : slab_need(p.T, p.out, p.in, p.dtype); }
+size_t forward_need(const LinearProblem& p) { return linear_takes_few(p.T, p.out, p.in, p.dtype) ? 0 : product_need(p.T, p.out, p.in, p.dtype, false); }
 
 // The bias' partial sums are done with when the product's begin: one after the other on the stream they share the space.
 size_t backward_need(const LinearProblem& p, bool bias, bool input) {
   const size_t sums = bias ? static_cast<size_t>(linear_parts(p.T, p.out, p.dtype, device_compute_units())) * static_cast<size_t>(norm_pitch(p.out)) * 4u : 0;
-  const size_t slabs = input ? slab_need(p.T, p.in, p.out, p.dtype) : 0;
-  return sums > slabs ? sums : slabs;
+  const size_t product = input ? product_need(p.T, p.in, p.out, p.dtype, true) : 0;
+  return sums > product ? sums : product;
 }
 
 bool matrix_ok(int64_t rows, int64_t cols) {

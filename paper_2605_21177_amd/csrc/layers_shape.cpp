@@ -89,29 +89,46 @@ int64_t linear_parts(int64_t T, int64_t out, int dtype, int compute_units) {
   return want < 1 ? 1 : want < need ? want : need;
 }
 
+// bf16 rows that are no 16-byte pieces go through registers, in 128-wide tiles, at 1.6 times the rounds' time, or are copied first, in a
+// launch and at 7 TB/s.  us, through registers / copied: 1001 x 2907 x 2705 47 / 39, 4095 x 4097 x 4095 190 and 259 / 125 and 179 (dX),
+// 2047 x 1023 x 1025 25 / 21; 300 x 2051 x 2051 20 / 23, 64 x 4097 x 4095 21 / 29.  Rows of pieces that are no whole lines stay where they are:
+// 4096 x 4104 x 4096 113 / 124.  fp32 always goes through registers, in 64- and 128-wide tiles.
 LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, int dtype, int compute_units) {
   const int64_t unit = dtype == 0 ? 32 : 64;                 // k of a stage: slabs are whole stages
-  // rows without 16-byte pieces go through registers, in 128-wide tiles (fp32 always does, in 64- and 128-wide ones)
-  const bool direct = K % 8 == 0 && N % 8 == 0;
-  const int first = dtype == 0 || direct ? 64 : 128, last = dtype != 0 && direct ? 256 : 128;
-  LinearPlan best{first, 1, K};
+  const bool pieces = dtype == 0 || (K % 8 == 0 && N % 8 == 0);
+  const double elements = ((double)M + (double)N) * (double)K;
+  LinearPlan best{dtype == 0 ? 64 : 128, 1, K, false};
   double least = -1;
-  for (int tile = first; tile <= last; tile *= 2) {
-    const double tiles = (double)ceil_div(M, tile) * (double)ceil_div(N, dtype != 0 && tile == 64 ? 128 : tile);
-    for (int want = 1; want <= 16; ++want) {
-      const int64_t ks = ceil_div(ceil_div(K, want), unit) * unit;
-      const int64_t slabs = ceil_div(K, ks);
-      if (slabs != want || (want > 1 && ks < 256)) continue;
-      double cost = round_cost(dtype, tile, tiles * (double)slabs, (double)ks, compute_units);
-      if (!direct && dtype != 0) cost *= 1.6;                // 1001 x 2907 x 2705: 51 us where the direct loads' rule says 32
-      if (slabs > 1) cost += 3 + (8.0 * (double)slabs + 4) * (double)M * (double)N / 7e6;
-      if (least < 0 || cost < least) {
-        least = cost;
-        best = LinearPlan{tile, (int32_t)slabs, slabs > 1 ? ks : K};
+  for (int pack = 0; pack <= (!pieces && elements < 1e12 ? 1 : 0); ++pack) {
+    const bool direct = dtype != 0 && (pieces || pack);
+    for (int tile = dtype == 0 || direct ? 64 : 128; tile <= (direct ? 256 : 128); tile *= 2) {
+      const double tiles = (double)ceil_div(M, tile) * (double)ceil_div(N, dtype != 0 && tile == 64 ? 128 : tile);
+      for (int want = 1; want <= 16; ++want) {
+        const int64_t ks = ceil_div(ceil_div(K, want), unit) * unit;
+        const int64_t slabs = ceil_div(K, ks);
+        if (slabs != want || (want > 1 && ks < 256)) continue;
+        double cost = round_cost(dtype, tile, tiles * (double)slabs, (double)ks, compute_units);
+        if (dtype != 0 && !direct) cost *= 1.6;
+        if (pack) cost += 4 + 4 * elements / 7e6;
+        if (slabs > 1) cost += 3 + (8.0 * (double)slabs + 4) * (double)M * (double)N / 7e6;
+        if (least < 0 || cost < least) {
+          least = cost;
+          best = LinearPlan{tile, (int32_t)slabs, slabs > 1 ? ks : K, pack != 0};
+        }
       }
     }
   }
   return best;
+}
+
+LinearSpace linear_space(const LinearPlan& plan, int64_t M, int64_t N, int64_t K, bool across) {
+  LinearSpace l{0, 0, 0};
+  if (plan.slabs > 1) l.slabs = (size_t)plan.slabs * (size_t)M * (size_t)norm_pitch(N) * 4u;
+  if (plan.pack) {
+    l.a = (size_t)M * (size_t)packed_pitch(K) * 2u;
+    l.b = across ? (size_t)packed_pitch(K) * (size_t)packed_pitch(N) * 2u : (size_t)N * (size_t)packed_pitch(K) * 2u;
+  }
+  return l;
 }
 
 // The pass over the weights against tiles and slabs: x is read again by every workgroup, and rows that are no 16-byte pieces in twice

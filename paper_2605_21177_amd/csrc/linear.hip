@@ -350,6 +350,40 @@ int join_slabs(const Slabs& s, int64_t M, int64_t N, const Epilogue& e, hipStrea
   return (int)hipGetLastError();
 }
 
+// An operand copied to rows of whole 128-byte lines, zero behind its rows and columns: 8 elements a lane, one operand per row of blocks.
+struct PackOne {
+  const unsigned short* from;
+  unsigned short* to;
+  int64_t ld, rows, cols, rows_p, pitch;
+};
+__global__ __launch_bounds__(256) void pack_kernel(const PackOne first, const PackOne second) {
+  const PackOne p = blockIdx.y == 0 ? first : second;
+  const int64_t per_row = p.pitch / 8, n = p.rows_p * per_row;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+    const int64_t r = i / per_row, c = i % per_row * 8;
+    Row<unsigned short> x;
+    x.zero();
+    if (r < p.rows && c < p.cols) x.load(p.from + r * p.ld + c, p.cols - c);
+    *(u32x4_t*)(p.to + i * 8) = x.v;
+  }
+}
+
+// Rows that the copies would not improve: whole lines, over whole stages of k.
+bool whole_lines(const void* p, int64_t ld, int64_t cols, int64_t K, bool across) {
+  return (uintptr_t)p % 128 == 0 && ld % 64 == 0 && K % 64 == 0 && direct_rows(p, ld, cols, across);
+}
+
+int launch_pack(const PackOne (&ones)[2], int n, hipStream_t st) {
+  if (n == 0) return 0;
+  int64_t most = 0;
+  for (int i = 0; i < n; ++i) {
+    const int64_t blocks = ceil_div(ones[i].rows_p * (ones[i].pitch / 8), 256);
+    if (blocks > most) most = blocks;
+  }
+  hipLaunchKernelGGL(pack_kernel, dim3((unsigned)(most < 16384 ? most : 16384), (unsigned)n), dim3(256), 0, st, ones[0], ones[n - 1]);
+  return (int)hipGetLastError();
+}
+
 template <int KB>
 int launch_product(const void* A, int64_t lda, const void* B, int64_t ldb, int64_t M, int64_t N, int64_t K, int dtype, const Epilogue& e,
                    float* ws, hipStream_t st) {
@@ -362,10 +396,31 @@ int launch_product(const void* A, int64_t lda, const void* B, int64_t ldb, int64
     else err = plan.tile == 128 ? launch_tiles_f32<128, 128, KB, false>(q, e, s, st) : launch_tiles_f32<64, 64, KB, false>(q, e, s, st);
     return err != 0 || plan.slabs == 1 ? err : join_slabs<float>(s, M, N, e, st);
   }
+  int64_t cols_b = KB ? N : K;
+  if (plan.pack) {
+    const LinearSpace l = linear_space(plan, M, N, K, KB != 0);
+    unsigned short* const to = (unsigned short*)((unsigned char*)ws + l.slabs);
+    PackOne ones[2];
+    int n = 0;
+    if (!whole_lines(A, lda, K, K, false)) {
+      ones[n++] = PackOne{(const unsigned short*)A, to, lda, M, K, M, packed_pitch(K)};
+      A = to;
+      lda = packed_pitch(K);
+    }
+    if (!whole_lines(B, ldb, cols_b, K, KB != 0)) {
+      unsigned short* const to_b = to + l.a / 2;
+      ones[n++] = PackOne{(const unsigned short*)B, to_b, ldb, KB ? K : N, cols_b, KB ? packed_pitch(K) : N, packed_pitch(cols_b)};
+      B = to_b;
+      ldb = cols_b = packed_pitch(cols_b);
+    }
+    err = launch_pack(ones, n, st);
+    if (err != 0) return err;
+    K = packed_pitch(K);                          // where it grows, both were copied
+  }
   const Product q{(const unsigned short*)A, (const unsigned short*)B, lda, ldb, M, N, K};
   // a slab of fewer k than a stage has nothing for the direct loads
   const int64_t last = plan.slabs > 1 ? K - (plan.slabs - 1) * plan.kslab : K;
-  const bool direct = direct_rows(A, lda, K, false) && direct_rows(B, ldb, N, KB != 0) && last >= Tile128::BK;
+  const bool direct = direct_rows(A, lda, K, false) && direct_rows(B, ldb, cols_b, KB != 0) && last >= Tile128::BK;
   auto by_split = [&](auto split) {
     constexpr bool S = decltype(split)::value != 0;
     if (!direct) return launch_tiles<Tile128, KB, THROUGH_REGISTERS, S>(q, e, s, st);

@@ -136,3 +136,27 @@ def test_two_streams_at_once_with_workspaces_of_their_own():
     torch.cuda.synchronize()
     for (_, a, _), (_, b, _) in zip(alone, both):
         assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+@pytest.mark.parametrize("T,n_in,out,pad,lead", [(2047, 1023, 1025, 0, 0), (2000, 500, 500, 12, 4), (1500, 1001, 1200, 7, 1), (1500, 1024, 1201, 0, 0), (3001, 1090, 1100, 2, 3)])
+def test_linear_rows_without_pieces(T, n_in, out, pad, lead):
+    """bf16 rows at odd places, copied or not, inside buffers that hold no numbers elsewhere; a workspace that holds none either."""
+    gen = torch.Generator(device=DEV).manual_seed(T + n_in + out)
+
+    def inside(t):
+        rows, cols = t.shape
+        v = torch.full((lead + rows * (cols + pad) + 64,), float("nan"), dtype=torch.bfloat16, device=DEV)[lead:lead + rows * (cols + pad)].view(rows, cols + pad)[:, :cols]
+        return v.copy_(t)
+
+    def ws(n):
+        return torch.full((n // 4,), float("nan"), device=DEV) if n else None
+
+    x, W, dy = inside(_randn(gen, T, n_in)), inside(_randn(gen, out, n_in) / n_in ** 0.5), inside(_randn(gen, T, out))
+    y, dx = inside(torch.zeros(T, out, device=DEV)), inside(torch.zeros(T, n_in, device=DEV))
+    layer = B.make_linear(x, W)
+    B.chunkft_linear_forward(layer, y, ws=ws(B.chunkft_linear_workspace_bytes(layer)))
+    _close(y, x.double() @ W.double().t(), x.double().abs() @ W.double().abs().t(), n_in + 4, "y")
+    layer, db = B.make_linear(None, W, tokens=T), torch.empty(out, device=DEV)
+    B.chunkft_linear_backward(layer, dy, dX=dx, db=db, ws=ws(B.chunkft_linear_workspace_bytes(layer, backward=True)))
+    _close(dx, dy.double() @ W.double(), dy.double().abs() @ W.double().abs(), out + 4, "dx")
+    _close(db, dy.double().sum(0), dy.double().abs().sum(0), T + 4, "db")
