@@ -351,6 +351,7 @@ int join_slabs(const Slabs& s, int64_t M, int64_t N, const Epilogue& e, hipStrea
 }
 
 // An operand copied to rows of whole 128-byte lines, zero behind its rows and columns: 8 elements a lane, one operand per row of blocks.
+// Bound by the loads at 2-byte addresses: 1001 x 2907 and 2705 x 2907 10 us, 4.3 TB/s (the same without the division of the index).
 struct PackOne {
   const unsigned short* from;
   unsigned short* to;
