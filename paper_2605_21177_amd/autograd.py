@@ -33,7 +33,7 @@ class ChunkSegment:
 
     Plain mode (`g` given): backward writes the segment's fp32 gradient to `g`
     (`end - begin` elements) on the first micro-batch after `reset()` and adds to
-    it on the following ones.
+    it on the following ones. A layer's backward that runs out of memory changes and counts nothing.
     Fused mode (`master`, `m`, `v`, `hp` given): backward updates the chunk state
     and the segment of `W` in place (a bf16 `W` receives the rounded master, an fp32
     `W` a copy of it; `master` may also be the segment of an fp32 `W` itself, the
@@ -82,11 +82,13 @@ class ChunkSegment:
             self._ws = torch.empty(need, dtype=torch.uint8, device="cuda")
         return self._ws
 
+    def check_open(self) -> None:
+        """Fused mode takes one backward pass per optimizer step."""
+        if self.active and self.fused and self.micro_batches:
+            raise RuntimeError("fused mode takes one micro-batch per optimizer step")
 
     def one_more(self) -> None:
-        """Counts a backward pass; fused mode takes one per optimizer step."""
-        if self.fused and self.micro_batches:
-            raise RuntimeError("fused mode takes one micro-batch per optimizer step")
+        """Counts a backward pass, behind the calls that it made: one that failed leaves the segment as it was, to be repeated."""
         self.micro_batches += 1
 
 
@@ -95,26 +97,32 @@ def _scratch(need: int, device):
     return torch.empty(need, dtype=torch.uint8, device=device) if need else None
 
 
-def _weight_gradient(seg: ChunkSegment, X, dY, W) -> None:
-    """The segment's gradient of y = x W^T, to where it goes; X [T, in] and dY [T, out]."""
+def _weight_gradient(seg: ChunkSegment, X, dY, W):
+    """The segment's gradient of y = x W^T, to where it goes; X [T, in] and dY [T, out]. What the calls need is allocated here;
+    what is returned makes them, and counts them once they are made."""
     out, n_in = W.shape
+    seg.check_open()
     layer = B.make_layer(B.LINEAR, X, dY, out, n_in, split_k=seg.split_k)
-    muon = seg.fused and isinstance(seg.hp, B.MuonHparams)
-    first = seg.micro_batches == 0
-    seg.one_more()
     ws = seg.workspace(layer)
+    muon = seg.fused and isinstance(seg.hp, B.MuonHparams)
     if muon:
         rows = (seg.end - seg.begin) // n_in
         g = torch.empty(seg.end - seg.begin, dtype=torch.float32, device=W.device)
-        B.chunkft_chunk_wgrad(layer, seg.begin, seg.end, g, ws=ws)
-        need = B.chunkft_orthogonalize_workspace_bytes(seg.hp.precision, rows, n_in)
-        B.chunkft_muon_chunk(g, seg.master, seg.m, W.view(-1)[seg.begin:seg.end], rows, n_in, seg.hp,
-                             w_dtype=B._torch_dtype_code(W), ws=_scratch(need, W.device))
-    elif seg.fused:
-        # W is what the next forward multiplies with: it always receives the update
-        B.chunkft_wgrad_adamw_fused(layer, seg.begin, seg.end, W, seg.master, seg.m, seg.v, seg.hp, ws=ws)
-    else:
-        B.chunkft_chunk_wgrad(layer, seg.begin, seg.end, seg.g, accumulate=not first, ws=ws)
+        muon_ws = _scratch(B.chunkft_orthogonalize_workspace_bytes(seg.hp.precision, rows, n_in), W.device)
+
+    def run():
+        if muon:
+            B.chunkft_chunk_wgrad(layer, seg.begin, seg.end, g, ws=ws)
+            B.chunkft_muon_chunk(g, seg.master, seg.m, W.view(-1)[seg.begin:seg.end], rows, n_in, seg.hp,
+                                 w_dtype=B._torch_dtype_code(W), ws=muon_ws)
+        elif seg.fused:
+            # W is what the next forward multiplies with: it always receives the update
+            B.chunkft_wgrad_adamw_fused(layer, seg.begin, seg.end, W, seg.master, seg.m, seg.v, seg.hp, ws=ws)
+        else:
+            B.chunkft_chunk_wgrad(layer, seg.begin, seg.end, seg.g, accumulate=seg.micro_batches > 0, ws=ws)
+        seg.one_more()
+
+    return run
 
 
 class _VectorGrads:
@@ -144,13 +152,12 @@ class _VectorGrads:
         for (seg, vec), buf in zip(self.pairs, self.bufs):
             if buf is None:
                 continue
-            first = seg.micro_batches == 0
-            seg.one_more()
             if seg.fused:
                 B.chunkft_adamw_chunk(buf, seg.master, seg.m, seg.v, vec[seg.begin:seg.end], seg.end - seg.begin, seg.hp,
                                       w_dtype=B._torch_dtype_code(vec))
             elif not self.direct:
-                seg.g.copy_(buf) if first else seg.g.add_(buf)
+                seg.g.add_(buf) if seg.micro_batches else seg.g.copy_(buf)
+            seg.one_more()
 
 
 class _ChunkLinear(torch.autograd.Function):
@@ -167,7 +174,7 @@ class _ChunkLinear(torch.autograd.Function):
         # the input gradient uses W as it was in the forward pass: enqueue it before any update
         dx = dy.matmul(W) if ctx.needs_input_grad[0] else None
         if seg is not None and seg.active:
-            _weight_gradient(seg, _as_rows(x, W.shape[1]), _as_rows(dy, W.shape[0]), W)
+            _weight_gradient(seg, _as_rows(x, W.shape[1]), _as_rows(dy, W.shape[0]), W)()
         return dx, None, None, None
 
 
@@ -196,6 +203,7 @@ class _LinearLayer(torch.autograd.Function):
         dx = torch.empty(T, n_in, dtype=W.dtype, device=W.device) if ctx.needs_input_grad[0] else None
         grads = _VectorGrads([(ctx.bias_seg, bias)], W.device)
         dz = torch.empty_like(z) if z is not None else dy2
+        weight = _weight_gradient(ctx.seg, x2, dz, W) if T and ctx.seg is not None and ctx.seg.active else None
         if T == 0:
             _no_tokens([ctx.seg, ctx.bias_seg])
         elif z is not None or dx is not None or grads.bufs[0] is not None:
@@ -206,8 +214,8 @@ class _LinearLayer(torch.autograd.Function):
                                       accumulate=grads.accumulate, ws=ws)
         if T:
             grads.finish()
-            if ctx.seg is not None and ctx.seg.active:
-                _weight_gradient(ctx.seg, x2, dz, W)
+            if weight is not None:
+                weight()
         return (None if dx is None else dx.view(ctx.shape), None, None, dy if ctx.needs_input_grad[3] else None, None, None, None,
                 None, None)
 
@@ -253,8 +261,8 @@ def _as_rows(t, width: int):
 def _open(segs) -> None:
     """Before anything is enqueued: fused segments have not been updated in this step."""
     for seg in segs:
-        if seg is not None and seg.active and seg.fused and seg.micro_batches:
-            raise RuntimeError("fused mode takes one micro-batch per optimizer step")
+        if seg is not None:
+            seg.check_open()
 
 
 def _no_tokens(segs) -> None:
