@@ -79,21 +79,25 @@ constexpr int kGateLanes = 32, kGateRows = 8;       // of the pass over dy and z
 // Rows of partial sums (of norm_pitch(out) floats) that a backward pass leaves for the bias.
 int64_t linear_parts(int64_t T, int64_t out, int dtype, int compute_units);
 
-// How a product [M, K] x [K, N] is cut: square tiles of `tile` (bf16: 64 is 64 x 128), `slabs` runs of kslab values of k.  From the shape alone: the workspace
-// that the caller gives depends on it.
+// How a product [M, K] x [K, N] is cut: square tiles of `tile` (bf16: 64 is 64 x 128), `slabs` runs of kslab values of k.
 struct LinearPlan {
   int32_t tile, slabs;
   int64_t kslab;
   bool pack;            // operands are copied to rows of whole 128-byte lines, first, where they are not so already
 };
-LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, int dtype, int compute_units);
-// Rows and elements of a row of a packed operand (whole stages of k, whole lines), and bytes of a plan's parts of the workspace, in this
-// order: the slabs' sums, A [M, K], B ([N, K], or [K, N] across).
+// How its operands come: in rows of 16-byte pieces, which the direct loads take (bf16), through registers, or copied to such rows.
+enum LinearRows : int { ROWS_IN_PIECES = 0, ROWS_AS_THEY_LIE = 1, ROWS_COPIED = 2 };
+LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, int dtype, int compute_units, LinearRows rows = ROWS_IN_PIECES);
+// What a call runs by.  pieces: both operands' rows, with their addresses and strides, are such as the direct loads take; across: B
+// is [K, N] (otherwise [N, K]).
+LinearPlan linear_choice(int64_t M, int64_t N, int64_t K, int dtype, int compute_units, bool across, bool pieces);
+// Rows and elements of a row of a packed operand (whole stages of k, whole lines), and bytes of the workspace's parts, in this order: the
+// slabs' sums, A [M, K], B ([N, K], or [K, N] across).  From the shape alone: they are enough for either choice.
 inline int64_t packed_pitch(int64_t n) { return (n + 63) / 64 * 64; }
 struct LinearSpace {
   size_t slabs, a, b;
 };
-LinearSpace linear_space(const LinearPlan& plan, int64_t M, int64_t N, int64_t K, bool across);
+LinearSpace linear_space(int64_t M, int64_t N, int64_t K, int dtype, int compute_units, bool across);
 bool linear_takes_few(int64_t T, int64_t out, int64_t in, int dtype);   // the forward pass is one pass over the weights, whatever the plan
 
 int launch_linear_forward(const LinearProblem& p, void* Y, int64_t ldy, void* Z, int64_t ldz, float* ws, void* stream);

@@ -70,7 +70,7 @@ int check_linear(const chunkft_linear* L, LinearProblem* p) {
 
 // A product's slabs and packed operands.
 size_t product_need(int64_t M, int64_t N, int64_t K, int32_t dtype, bool across) {
-  const LinearSpace l = linear_space(linear_plan(M, N, K, dtype, device_compute_units()), M, N, K, across);
+  const LinearSpace l = linear_space(M, N, K, dtype, device_compute_units(), across);
   return l.slabs + l.a + l.b;
 }
 

@@ -89,42 +89,67 @@ int64_t linear_parts(int64_t T, int64_t out, int dtype, int compute_units) {
   return want < 1 ? 1 : want < need ? want : need;
 }
 
-// bf16 rows that are no 16-byte pieces go through registers, in 128-wide tiles, at 1.6 times the rounds' time, or are copied first, in a
-// launch and at 7 TB/s.  us, through registers / copied: 1001 x 2907 x 2705 47 / 39, 4095 x 4097 x 4095 190 and 259 / 125 and 179 (dX),
-// 2047 x 1023 x 1025 25 / 21; 300 x 2051 x 2051 20 / 23, 64 x 4097 x 4095 21 / 29.  Rows of pieces that are no whole lines stay where they are:
-// 4096 x 4104 x 4096 113 / 124.  fp32 always goes through registers, in 64- and 128-wide tiles.
-LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, int dtype, int compute_units) {
+namespace {
+
+struct Cut {
+  LinearPlan plan;
+  double cost;          // us
+};
+
+// The cheapest of the tiles and slabs that a way of taking the operands has.  Through registers a bf16 product has 128-wide tiles and
+// takes 1.6 times the rounds' time; fp32 always goes that way, in 64- and 128-wide tiles.
+Cut best_cut(int64_t M, int64_t N, int64_t K, int dtype, int compute_units, LinearRows rows) {
   const int64_t unit = dtype == 0 ? 32 : 64;                 // k of a stage: slabs are whole stages
-  const bool pieces = dtype == 0 || (K % 8 == 0 && N % 8 == 0);
-  const double elements = ((double)M + (double)N) * (double)K;
-  LinearPlan best{dtype == 0 ? 64 : 128, 1, K, false};
-  double least = -1;
-  for (int pack = 0; pack <= (!pieces && elements < 1e12 ? 1 : 0); ++pack) {
-    const bool direct = dtype != 0 && (pieces || pack);
-    for (int tile = dtype == 0 || direct ? 64 : 128; tile <= (direct ? 256 : 128); tile *= 2) {
-      const double tiles = (double)ceil_div(M, tile) * (double)ceil_div(N, dtype != 0 && tile == 64 ? 128 : tile);
-      for (int want = 1; want <= 16; ++want) {
-        const int64_t ks = ceil_div(ceil_div(K, want), unit) * unit;
-        const int64_t slabs = ceil_div(K, ks);
-        if (slabs != want || (want > 1 && ks < 256)) continue;
-        double cost = round_cost(dtype, tile, tiles * (double)slabs, (double)ks, compute_units);
-        if (dtype != 0 && !direct) cost *= 1.6;
-        if (pack) cost += 4 + 4 * elements / 7e6;
-        if (slabs > 1) cost += 3 + (8.0 * (double)slabs + 4) * (double)M * (double)N / 7e6;
-        if (least < 0 || cost < least) {
-          least = cost;
-          best = LinearPlan{tile, (int32_t)slabs, slabs > 1 ? ks : K, pack != 0};
-        }
-      }
+  const bool direct = dtype != 0 && rows != ROWS_AS_THEY_LIE;
+  if (rows == ROWS_COPIED) K = packed_pitch(K);
+  Cut best{LinearPlan{dtype == 0 ? 64 : 128, 1, K, rows == ROWS_COPIED}, -1};
+  for (int tile = dtype == 0 || direct ? 64 : 128; tile <= (direct ? 256 : 128); tile *= 2) {
+    const double tiles = (double)ceil_div(M, tile) * (double)ceil_div(N, dtype != 0 && tile == 64 ? 128 : tile);
+    for (int want = 1; want <= 16; ++want) {
+      const int64_t ks = ceil_div(ceil_div(K, want), unit) * unit;
+      const int64_t slabs = ceil_div(K, ks);
+      if (slabs != want || (want > 1 && ks < 256)) continue;
+      if (direct && want > 1 && K - (slabs - 1) * ks < unit) continue;       // a slab of no whole stage has nothing for the direct loads
+      double cost = round_cost(dtype, tile, tiles * (double)slabs, (double)ks, compute_units);
+      if (dtype != 0 && !direct) cost *= 1.6;
+      if (slabs > 1) cost += 3 + (8.0 * (double)slabs + 4) * (double)M * (double)N / 7e6;
+      if (best.cost < 0 || cost < best.cost) best = Cut{LinearPlan{tile, (int32_t)slabs, slabs > 1 ? ks : K, rows == ROWS_COPIED}, cost};
     }
   }
   return best;
 }
 
-LinearSpace linear_space(const LinearPlan& plan, int64_t M, int64_t N, int64_t K, bool across) {
+// Rows of a shape that the direct loads take wherever they begin on 16 bytes: along k they may end anywhere, across k in whole pieces.
+// (Rows along k that are no whole pieces are no neighbours either; only a stride of their own makes them so.)
+bool shape_in_pieces(int64_t N, int64_t K, bool across) { return K % 8 == 0 && (!across || N % 8 == 0); }
+
+}  // namespace
+
+LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, int dtype, int compute_units, LinearRows rows) {
+  return best_cut(M, N, K, dtype, compute_units, rows).plan;
+}
+
+// bf16 rows that are no 16-byte pieces go through registers or are copied first, in a launch and at 7 TB/s.  us, through registers
+// / copied: 1001 x 2907 x 2705 47 / 39, 4095 x 4097 x 4095 190 and 259 / 125 and 179 (dX), 2047 x 1023 x 1025 25 / 21;
+// 300 x 2051 x 2051 20 / 23, 64 x 4097 x 4095 21 / 29.  Rows of pieces that are no whole lines stay where they are: 4096 x 4104 x 4096
+// 109 / 118, 512 x 1032 x 8192 20 / 26, 1024 x 4104 x 14336 101 / 131; of what was tried only many 128-wide tiles gain by copies
+// (4096 x 4104 x 4097, 17 x 17 of the 256-wide ones: 205 / 177).  Views of a shape in pieces that lie elsewhere go through registers: its
+// workspace has no room for copies.
+LinearPlan linear_choice(int64_t M, int64_t N, int64_t K, int dtype, int compute_units, bool across, bool pieces) {
+  if (dtype != 0 && pieces && K >= 64) return linear_plan(M, N, K, dtype, compute_units, ROWS_IN_PIECES);
+  const Cut lie = best_cut(M, N, K, dtype, compute_units, ROWS_AS_THEY_LIE);
+  if (dtype == 0 || pieces || shape_in_pieces(N, K, across)) return lie.plan;
+  const Cut copied = best_cut(M, N, K, dtype, compute_units, ROWS_COPIED);
+  const double elements = ((double)M + (double)N) * (double)K;
+  return elements < 1e12 && copied.cost + 4 + 4 * elements / 7e6 < lie.cost ? copied.plan : lie.plan;
+}
+
+LinearSpace linear_space(int64_t M, int64_t N, int64_t K, int dtype, int compute_units, bool across) {
   LinearSpace l{0, 0, 0};
-  if (plan.slabs > 1) l.slabs = (size_t)plan.slabs * (size_t)M * (size_t)norm_pitch(N) * 4u;
-  if (plan.pack) {
+  const LinearPlan pieces = linear_plan(M, N, K, dtype, compute_units, ROWS_IN_PIECES), other = linear_choice(M, N, K, dtype, compute_units, across, false);
+  const int32_t slabs = pieces.slabs > other.slabs ? pieces.slabs : other.slabs;
+  if (slabs > 1) l.slabs = (size_t)slabs * (size_t)M * (size_t)norm_pitch(N) * 4u;
+  if (other.pack) {
     l.a = (size_t)M * (size_t)packed_pitch(K) * 2u;
     l.b = across ? (size_t)packed_pitch(K) * (size_t)packed_pitch(N) * 2u : (size_t)N * (size_t)packed_pitch(K) * 2u;
   }

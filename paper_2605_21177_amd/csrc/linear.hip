@@ -388,7 +388,9 @@ int launch_pack(const PackOne (&ones)[2], int n, hipStream_t st) {
 template <int KB>
 int launch_product(const void* A, int64_t lda, const void* B, int64_t ldb, int64_t M, int64_t N, int64_t K, int dtype, const Epilogue& e,
                    float* ws, hipStream_t st) {
-  const LinearPlan plan = linear_plan(M, N, K, dtype, device_compute_units());
+  int64_t cols_b = KB ? N : K;
+  const bool pieces = direct_rows(A, lda, K, false) && direct_rows(B, ldb, cols_b, KB != 0);
+  const LinearPlan plan = linear_choice(M, N, K, dtype, device_compute_units(), KB != 0, pieces);
   const Slabs s{plan.kslab, norm_pitch(N), ws, plan.slabs};
   int err;
   if (dtype == 0) {
@@ -397,9 +399,8 @@ int launch_product(const void* A, int64_t lda, const void* B, int64_t ldb, int64
     else err = plan.tile == 128 ? launch_tiles_f32<128, 128, KB, false>(q, e, s, st) : launch_tiles_f32<64, 64, KB, false>(q, e, s, st);
     return err != 0 || plan.slabs == 1 ? err : join_slabs<float>(s, M, N, e, st);
   }
-  int64_t cols_b = KB ? N : K;
   if (plan.pack) {
-    const LinearSpace l = linear_space(plan, M, N, K, KB != 0);
+    const LinearSpace l = linear_space(M, N, K, dtype, device_compute_units(), KB != 0);
     unsigned short* const to = (unsigned short*)((unsigned char*)ws + l.slabs);
     PackOne ones[2];
     int n = 0;
@@ -419,9 +420,7 @@ int launch_product(const void* A, int64_t lda, const void* B, int64_t ldb, int64
     K = packed_pitch(K);                          // where it grows, both were copied
   }
   const Product q{(const unsigned short*)A, (const unsigned short*)B, lda, ldb, M, N, K};
-  // a slab of fewer k than a stage has nothing for the direct loads
-  const int64_t last = plan.slabs > 1 ? K - (plan.slabs - 1) * plan.kslab : K;
-  const bool direct = direct_rows(A, lda, K, false) && direct_rows(B, ldb, cols_b, KB != 0) && last >= Tile128::BK;
+  const bool direct = direct_rows(A, lda, K, false) && direct_rows(B, ldb, cols_b, KB != 0) && K >= Tile128::BK;
   auto by_split = [&](auto split) {
     constexpr bool S = decltype(split)::value != 0;
     if (!direct) return launch_tiles<Tile128, KB, THROUGH_REGISTERS, S>(q, e, s, st);
