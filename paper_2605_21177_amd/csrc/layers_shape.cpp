@@ -97,7 +97,7 @@ struct Cut {
 };
 
 // The cheapest of the tiles and slabs that a way of taking the operands has.  Through registers a bf16 product has 128-wide tiles and
-// takes 1.6 times the rounds' time; fp32 always goes that way, in 64- and 128-wide tiles.
+// takes 1.75 times the rounds' time; fp32 always goes that way, in 64- and 128-wide tiles.
 Cut best_cut(int64_t M, int64_t N, int64_t K, int dtype, int compute_units, LinearRows rows) {
   const int64_t unit = dtype == 0 ? 32 : 64;                 // k of a stage: slabs are whole stages
   const bool direct = dtype != 0 && rows != ROWS_AS_THEY_LIE;
@@ -111,7 +111,7 @@ Cut best_cut(int64_t M, int64_t N, int64_t K, int dtype, int compute_units, Line
       if (slabs != want || (want > 1 && ks < 256)) continue;
       if (direct && want > 1 && K - (slabs - 1) * ks < unit) continue;       // a slab of no whole stage has nothing for the direct loads
       double cost = round_cost(dtype, tile, tiles * (double)slabs, (double)ks, compute_units);
-      if (dtype != 0 && !direct) cost *= 1.6;
+      if (dtype != 0 && !direct) cost *= 1.75;
       if (slabs > 1) cost += 3 + (8.0 * (double)slabs + 4) * (double)M * (double)N / 7e6;
       if (best.cost < 0 || cost < best.cost) best = Cut{LinearPlan{tile, (int32_t)slabs, slabs > 1 ? ks : K, rows == ROWS_COPIED}, cost};
     }
@@ -129,19 +129,22 @@ LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, int dtype, int compute_u
   return best_cut(M, N, K, dtype, compute_units, rows).plan;
 }
 
-// bf16 rows that are no 16-byte pieces go through registers or are copied first, in a launch and at 7 TB/s.  us, through registers
-// / copied: 1001 x 2907 x 2705 47 / 39, 4095 x 4097 x 4095 190 and 259 / 125 and 179 (dX), 2047 x 1023 x 1025 25 / 21;
-// 300 x 2051 x 2051 20 / 23, 64 x 4097 x 4095 21 / 29.  Rows of pieces that are no whole lines stay where they are: 4096 x 4104 x 4096
-// 109 / 118, 512 x 1032 x 8192 20 / 26, 1024 x 4104 x 14336 101 / 131; of what was tried only many 128-wide tiles gain by copies
-// (4096 x 4104 x 4097, 17 x 17 of the 256-wide ones: 205 / 177).  Views of a shape in pieces that lie elsewhere go through registers: its
-// workspace has no room for copies.
+// bf16 rows that are no 16-byte pieces go through registers or are copied first, in a launch and at 7 TB/s (A only where k is no whole
+// stages), unless the copies are mostly padding.  us, through registers / copied: 1001 x 2907 x 2705 47 / 39, 4095 x 4097 x 4095 190 and 259
+// / 125 and 179 (dX), 2047 x 1023 x 1025 25 / 21, 290 x 7188 x 1607 38 / 32; 300 x 2051 x 2051 20 / 23, 64 x 4097 x 4095 21 / 29; padded from 3 to
+// 64, 10^6 x 64 x 3 118 / 109.  Rows of pieces that are no whole lines stay where they are: 4096 x 4104 x 4096 109 / 118, 512 x 1032 x 8192
+// 20 / 26, 1024 x 4104 x 14336 101 / 131; of what was tried only many 128-wide tiles gain by copies (4096 x 4104 x 4097, 17 x 17 of the
+// 256-wide ones: 205 / 177).  Views of a shape in pieces that lie elsewhere go through registers: its workspace has no room for copies.
 LinearPlan linear_choice(int64_t M, int64_t N, int64_t K, int dtype, int compute_units, bool across, bool pieces) {
   if (dtype != 0 && pieces && K >= 64) return linear_plan(M, N, K, dtype, compute_units, ROWS_IN_PIECES);
   const Cut lie = best_cut(M, N, K, dtype, compute_units, ROWS_AS_THEY_LIE);
   if (dtype == 0 || pieces || shape_in_pieces(N, K, across)) return lie.plan;
   const Cut copied = best_cut(M, N, K, dtype, compute_units, ROWS_COPIED);
-  const double elements = ((double)M + (double)N) * (double)K;
-  return elements < 1e12 && copied.cost + 4 + 4 * elements / 7e6 < lie.cost ? copied.plan : lie.plan;
+  const double m = (double)M, n = (double)N, k = (double)K, kp = (double)packed_pitch(K);
+  const double read = (K % 64 != 0 ? m * k : 0) + n * k;
+  const double written = (K % 64 != 0 ? m * kp : 0) + (across ? kp * (double)packed_pitch(N) : n * kp);
+  if (written > 2 * read || written > 1e12) return lie.plan;
+  return copied.cost + 4 + 2 * (read + written) / 7e6 < lie.cost ? copied.plan : lie.plan;
 }
 
 LinearSpace linear_space(int64_t M, int64_t N, int64_t K, int dtype, int compute_units, bool across) {

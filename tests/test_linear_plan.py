@@ -48,3 +48,11 @@ def test_host_code_of_the_plan_under_sanitizers(tmp_path):
     assert r.returncode == 0, r.stderr[-2000:]
     r = subprocess.run([exe], capture_output=True, text=True, timeout=300)
     assert r.returncode == 0 and r.stdout.startswith("ok:"), (r.stdout[-1000:], r.stderr[-3000:])
+
+
+@pytest.mark.parametrize("backward", [0, 1])
+@pytest.mark.parametrize("T,n_in,out", [(1000000, 3, 64), (1000000, 64, 3), (1 << 24, 1, 1), (100000, 17, 1000), (200000, 33, 31), (65536, 9, 4097)])
+def test_operands_are_not_copied_into_rows_that_are_mostly_padding(T, n_in, out, backward):
+    """The space is at most twice the operands and the sums over the tokens or the slabs (which are few where the tokens are many)."""
+    operands = 2 * (T * (out if backward else n_in) + out * n_in)
+    assert _space(T, n_in, out, backward) <= 2 * operands + (2 << 20)
