@@ -47,15 +47,30 @@ __device__ __forceinline__ float normal_cdf<float>(float z, float& bell) {
   return z < 0.f ? tail : 1.f - tail;
 }
 
-// v_exp_f32 and v_rcp_f32 are good to one step of the result: three roundings of 2^-23 instead of one
-__device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.44269504f * z)); }
+// 1 / (1 + e^-z), and what is left of one beside it, from e^-|z|: neither is the difference of two numbers near each other.
+template <typename T>
+__device__ __forceinline__ float sigmoid(float z, float& rest) {
+  float e, r;
+  if constexpr (__is_same(T, float)) {
+    e = expf(-fabsf(z));
+    r = 1.f / (1.f + e);
+  } else {
+    // v_exp_f32 and v_rcp_f32 are good to one step of the result; the exponent is rounded before, so that the whole is off by
+    // (8 + 1.3 |z|) 2^-24.  Below 2^-126 there is nothing.
+    e = __builtin_amdgcn_exp2f(-1.44269504f * fabsf(z));
+    r = __builtin_amdgcn_rcpf(1.f + e);
+  }
+  const float other = e * r;
+  rest = z < 0.f ? r : other;
+  return z < 0.f ? other : r;
+}
 
 template <typename T>
 __device__ __forceinline__ float activate(float z, int act) {
   if (act == ACT_RELU) return z > 0.f ? z : (z != z ? z : 0.f);
-  float bell;
-  if (act == ACT_GELU) return z * normal_cdf<T>(z, bell);
-  if (act == ACT_SILU) return z * sigmoid(z);
+  float beside;
+  if (act == ACT_GELU) return z * normal_cdf<T>(z, beside);
+  if (act == ACT_SILU) return z * sigmoid<T>(z, beside);
   return z;
 }
 
@@ -67,8 +82,9 @@ __device__ __forceinline__ float slope(float z, int act) {
     const float cdf = normal_cdf<T>(z, bell);
     return fmaf(0.39894228f * z, bell, cdf);
   }
-  const float s = sigmoid(z);
-  return s * fmaf(z, 1.f - s, 1.f);
+  float rest;
+  const float s = sigmoid<T>(z, rest);
+  return s * fmaf(z, rest, 1.f);
 }
 
 // What a product's row piece becomes: N consecutive columns of row m.

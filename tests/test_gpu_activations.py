@@ -63,3 +63,17 @@ def test_gelu_is_good_to_a_few_steps_of_its_value_far_out_too(dtype, tokens):
     cdf, bell = 0.5 * torch.special.erfc(-z / math.sqrt(2)), torch.exp(-z * z / 2) / math.sqrt(2 * math.pi)
     _within(y, z * cdf, (z * cdf).abs(), count, dt, "gelu")
     _within(dz, cdf + z * bell, cdf + z.abs() * bell, count, dt, "slope")
+
+
+@pytest.mark.parametrize("tokens", [1, 70])
+@pytest.mark.parametrize("dtype", sorted(DTYPES))
+def test_silu_is_good_to_a_few_steps_of_its_value_far_out_too(dtype, tokens):
+    """fp32: an exponential to 2 units, three roundings and the product: 8.  bf16: the exponent 1.44 |z| is rounded, 1.3 |z| on top."""
+    dt = DTYPES[dtype]
+    z = _values(-80, 80, 5001, dt)
+    y, dz = _run(z, B.ACT_SILU, tokens)
+    z = z.double()
+    count = 8 + 0 * z if dt is torch.float32 else 8 + 1.3 * z.abs()
+    s, rest = torch.sigmoid(z), torch.sigmoid(-z)
+    _within(y, z * s, (z * s).abs(), count, dt, "silu")
+    _within(dz, s * (1 + z * rest), s * (1 + z.abs() * rest), count, dt, "slope")
