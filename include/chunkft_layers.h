@@ -16,6 +16,7 @@
  * identical inputs giving identical bits, no exceptions.  Inputs and outputs of a call do not overlap unless it says so.
  * A workspace is scratch: calls that may overlap in time need workspaces of their own (so do graphs that may).
  * Types: CHUNKFT_BF16 or CHUNKFT_F32; every sum, statistic and state is fp32 (or wider), a result is rounded once, to nearest.
+ * What is rounded on the way besides: dz before its product with W, and the operands of the orthogonalisation's products (below).
  * A call whose launch would need 2^32 lanes or more is refused with ERR_HIP.
  * Any alignment of the element type is accepted; rows of 16 bytes at 16-byte addresses are fastest.
  */
@@ -68,8 +69,12 @@ int chunkft_norm_backward(const chunkft_norm* N, const float* stats, const void*
 
 /* ---------------------------------------------------------------------- linear layer
  *   z = x W^T + bias      y = act(z) + residual
- *   dz = dy act'(z)       db[j] = sum_t dz[t, j]       dx = dz W
- * act: NONE z;  RELU max(z, 0) (slope 0 at 0);  GELU z (1 + erf(z / sqrt 2)) / 2;  SILU z / (1 + exp(-z)).
+ *   dz = dy act'(z)       db[j] = sum_t dz[t, j]       dx = dz W, with dz as it is stored
+ * In bf16 with an activation dx therefore has two roundings: 2.35e-3 of its norm from the definition (14336 terms), which rounded
+ * once is 1.66e-3.
+ * act: NONE z;  RELU max(z, 0) (slope 0 at 0);  GELU z (1 + erf(z / sqrt 2)) / 2;  SILU z / (1 + exp(-z)).  GELU and SILU are good to
+ * 8 2^-24 of their value in fp32; in bf16, before the rounding, to (24 + 1.25 z^2) 2^-24 and (8 + 1.3 |z|) 2^-24, and zero where 2^-118 is
+ * more than the value.  At infinities the formulas' 0 times infinity is NaN: GELU and SILU at minus infinity, their slopes at both.
  * ---------------------------------------------------------------------- */
 typedef enum { CHUNKFT_ACT_NONE = 0, CHUNKFT_ACT_RELU = 1, CHUNKFT_ACT_GELU = 2, CHUNKFT_ACT_SILU = 3 } chunkft_activation;
 
@@ -115,7 +120,8 @@ int chunkft_linear_backward(const chunkft_linear* L, const void* dY, int64_t ldd
  * ---------------------------------------------------------------------- */
 
 /* Operands of the steps' products: CHUNKFT_BF16: 16 bits (11 of them digits), for results of that size; CHUNKFT_F32: 22 digits, three times
- * the work.  Sums are fp32 in both. */
+ * the work.  Sums are fp32 in both.  With 11 digits a bf16 result is 1.9e-3 of its norm from the definition, which rounded once is 1.66e-3; a
+ * bf16 matrix handed over as fp32 has 22.  X itself is held to no less than 2^-38: where eps is far above |U|, small results lose digits. */
 size_t chunkft_orthogonalize_workspace_bytes(int32_t precision, int64_t rows, int64_t cols);
 
 /* G (device, in), O (device, out)  rows x cols of `dtype`, which is also the precision; O may be G itself, with its row stride.

@@ -310,8 +310,8 @@ def chunk_linear(x: torch.Tensor, W: torch.Tensor, seg: Optional[ChunkSegment], 
     """`act(x @ W^T + bias) + residual` with the chunk-restricted weight gradient in backward.  `W` is
     `[out, in]` row-major on the GPU, bf16 or fp32, and must not require grad; nor must `bias`, a vector
     of `out` elements, whose active part `bias_seg` names.  `activation`: ACT_NONE, ACT_RELU, ACT_GELU
-    or ACT_SILU; `residual` has the output's shape and may require grad.  Without bias, activation and residual
-    the products are torch's."""
+    or ACT_SILU; `residual` has the output's shape and may require grad.  With an activation the input gradient is the product
+    of the pre-activation's gradient rounded to W's type.  Without bias, activation and residual the products are torch's."""
     if W.requires_grad:
         raise ValueError("W must not require grad: the dense weight gradient is never formed")
     if not W.is_contiguous():

@@ -3,7 +3,8 @@
 //   z = x W^T + b                      the product's epilogue adds the bias, keeps z where it is asked for, applies the activation
 //   y = act(z) + r                     and adds the residual, all on the fp32 sums; each result is rounded once
 //   dz = dy act'(z), db = sum_t dz     one pass over dy and z
-//   dx = dz W                          the product with W across k
+//   dx = dz W                          the product with W across k, of dz as it is stored: the matrix cores take bf16, and the weight's
+//                                      gradient is of the same dz (4096 x 4096 x 14336, GELU: 2.35e-3 off, 1.66e-3 from dz unrounded)
 #include <hip/hip_runtime.h>
 
 #include "internal.h"

@@ -77,3 +77,18 @@ def test_silu_is_good_to_a_few_steps_of_its_value_far_out_too(dtype, tokens):
     s, rest = torch.sigmoid(z), torch.sigmoid(-z)
     _within(y, z * s, (z * s).abs(), count, dt, "silu")
     _within(dz, s * (1 + z * rest), s * (1 + z.abs() * rest), count, dt, "slope")
+
+
+@pytest.mark.parametrize("dtype", sorted(DTYPES))
+@pytest.mark.parametrize("T,n_in,out", [(3, 40, 72), (200, 136, 520), (130, 201, 263), (300, 4096, 520)])
+def test_the_input_gradient_is_the_product_of_dz_as_it_is_stored(T, n_in, out, dtype):
+    """The same bits from dz handed in as the gradient of a layer without an activation."""
+    gen, dt = torch.Generator(device=DEV).manual_seed(T + out), DTYPES[dtype]
+    W, dy, z = (torch.randn(*s, generator=gen, device=DEV).to(dt) for s in ((out, n_in), (T, out), (T, out)))
+    dz, dx, again = torch.empty_like(dy), torch.empty(T, n_in, dtype=dt, device=DEV), torch.empty(T, n_in, dtype=dt, device=DEV)
+    for act, g, d, to in ((B.ACT_GELU, dy, dz, dx), (B.ACT_NONE, dz, None, again)):
+        layer = B.make_linear(None, W, activation=act, tokens=T)
+        need = B.chunkft_linear_workspace_bytes(layer, backward=True)
+        B.chunkft_linear_backward(layer, g, z, d, to, ws=torch.empty(need, dtype=torch.uint8, device=DEV))
+    torch.cuda.synchronize()
+    assert torch.equal(dx, again)
