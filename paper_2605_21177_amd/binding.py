@@ -90,12 +90,14 @@ class ScheduleEntry(C.Structure):
 class NormLayer(C.Structure):
     _fields_ = [("kind", C.c_int32), ("dtype", C.c_int32), ("T", C.c_int64), ("n", C.c_int64), ("X", C.c_void_p),
                 ("ldx", C.c_int64), ("w", C.c_void_p), ("b", C.c_void_p), ("eps", C.c_double)]
+    device = None          # of the tensors, where make_norm has seen them
 
 
 class LinearLayer(C.Structure):
     _fields_ = [("dtype", C.c_int32), ("activation", C.c_int32), ("out", C.c_int64), ("n_in", C.c_int64),
                 ("T", C.c_int64), ("X", C.c_void_p), ("ldx", C.c_int64), ("W", C.c_void_p), ("ldw", C.c_int64),
                 ("bias", C.c_void_p), ("residual", C.c_void_p), ("ldr", C.c_int64)]
+    device = None          # of the tensors, where make_linear has seen them
 
 
 class MuonHparams(C.Structure):
@@ -529,7 +531,16 @@ def _workspace(ws, dev: int):
 
 
 def _dtype_of(layer):
-    return _torch.float32 if layer.dtype == F32 else _torch.bfloat16
+    torch = _torch_module()
+    return torch.float32 if layer.dtype == F32 else torch.bfloat16
+
+
+def _device_of(layer) -> int:
+    """The current device, which has to be the one that the description's tensors were found on."""
+    dev = _torch_module().cuda.current_device()
+    if layer.device not in (None, dev):
+        raise ValueError("the layer's tensors must live on the current device")
+    return dev
 
 
 def make_norm(kind: int, X, w=None, b=None, eps: float = 1e-5) -> NormLayer:
@@ -540,7 +551,7 @@ def make_norm(kind: int, X, w=None, b=None, eps: float = 1e-5) -> NormLayer:
     n, dt, dev = X.shape[1], X.dtype, _torch.cuda.current_device()
     p, ld = _rows(X, "X", n, dt, dev)
     layer = NormLayer(kind, d, X.shape[0], n, p, ld, _vector(w, "w", n, dt, dev), _vector(b, "b", n, dt, dev), float(eps))
-    layer.tensors = X, w, b                                 # alive as long as the description is
+    layer.tensors, layer.device = (X, w, b), dev            # alive as long as the description is
     return layer
 
 
@@ -550,7 +561,7 @@ def chunkft_norm_workspace_bytes(layer: NormLayer) -> int:
 
 def chunkft_norm_forward(layer: NormLayer, Y, stats=None, stream=None, check: bool = True) -> int:
     """stats: None or a contiguous fp32 [tokens, 2] tensor (mean and reciprocal deviation of every token)."""
-    dev = _torch.cuda.current_device()
+    dev = _device_of(layer)
     p, ld = _rows(Y, "Y", layer.n, _dtype_of(layer), dev, layer.T)
     st = lib().chunkft_norm_forward(C.byref(layer), p, ld, _stats(stats, layer, dev), _stream_ptr(stream))
     if check and st != OK:
@@ -569,7 +580,7 @@ def _stats(stats, layer: NormLayer, dev: int):
 def chunkft_norm_backward(layer: NormLayer, stats, dY, dX=None, dw=None, w_range=None, db=None, b_range=None,
                           accumulate: bool = False, ws=None, stream=None, check: bool = True) -> int:
     """w_range, b_range: (begin, end) of the elements that dw and db hold (None: all)."""
-    T, dt, dev = layer.T, _dtype_of(layer), _torch.cuda.current_device()
+    T, dt, dev = layer.T, _dtype_of(layer), _device_of(layer)
     py, ldy = _rows(dY, "dY", layer.n, dt, dev, T)
     px, ldx = _rows(dX, "dX", layer.n, dt, dev, T)
     pw, pb = _grad_range(dw, "dw", w_range, layer.n, dev), _grad_range(db, "db", b_range, layer.n, dev)
@@ -593,7 +604,7 @@ def make_linear(X, W, bias=None, activation: int = ACT_NONE, residual=None, toke
         raise ValueError("give X or tokens")
     pr, ldr = _rows(residual, "residual", out, dt, dev, T)
     layer = LinearLayer(d, activation, out, n_in, T, px, ldx, pw, ldw, _vector(bias, "bias", out, dt, dev), pr, ldr)
-    layer.tensors = X, W, bias, residual                    # alive as long as the description is
+    layer.tensors, layer.device = (X, W, bias, residual), dev   # alive as long as the description is
     return layer
 
 
@@ -602,7 +613,7 @@ def chunkft_linear_workspace_bytes(layer: LinearLayer, backward: bool = False) -
 
 
 def chunkft_linear_forward(layer: LinearLayer, Y, Z=None, ws=None, stream=None, check: bool = True) -> int:
-    dt, dev = _dtype_of(layer), _torch.cuda.current_device()
+    dt, dev = _dtype_of(layer), _device_of(layer)
     st = lib().chunkft_linear_forward(C.byref(layer), *_rows(Y, "Y", layer.out, dt, dev, layer.T), *_rows(Z, "Z", layer.out, dt, dev, layer.T),
                                       *_workspace(ws, dev), _stream_ptr(stream))
     if check and st != OK:
@@ -613,7 +624,7 @@ def chunkft_linear_forward(layer: LinearLayer, Y, Z=None, ws=None, stream=None, 
 def chunkft_linear_backward(layer: LinearLayer, dY, Z=None, dZ=None, dX=None, db=None, b_range=None, accumulate: bool = False,
                             ws=None, stream=None, check: bool = True) -> int:
     """Without an activation Z and dZ are ignored (dz is dY).  b_range: (begin, end) of the elements that db holds (None: all)."""
-    dt, T, dev = _dtype_of(layer), layer.T, _torch.cuda.current_device()
+    dt, T, dev = _dtype_of(layer), layer.T, _device_of(layer)
     if layer.activation == ACT_NONE:
         Z = dZ = None
     st = lib().chunkft_linear_backward(C.byref(layer), *_rows(dY, "dY", layer.out, dt, dev, T), *_rows(Z, "Z", layer.out, dt, dev, T),
