@@ -33,22 +33,27 @@ double round_cost(int dtype, int tile, double items, double ks, double units) {
   return full * (pair * k + 1) + (rest > units ? pair * k + 1 : rest > 0 ? alone * k + 1 : 0);
 }
 
-// Time in us of `n` workgroups of a tile with ks values of k each.  Measured per 1024 k, one part / two: 128-wide tiles 10.2 / 19.5
-// alone on a compute unit and 14.5 / 38 the pair; 192-wide ones 12.5 / 31 where few units have one and 19.5 / 46 where all have;
-// 256-wide ones 18.5 / 51 and 26 / 70.  E.g. A for r = K = 4096, two parts: 228 us in 128-wide tiles (528 of them, two rounds), 186
-// in 192-wide (253, one round), 232 in 256-wide (136 on 256 units); r = 1024, K = 4096: 79 in one slab, 29 in four.
-double ns_rounds(int tile, int parts, double n, double ks, double units) {
-  const double k = ks / 1024;
-  if (tile == 128) {
-    const double pair = parts == 1 ? 14.5 : 38, alone = parts == 1 ? 10.2 : 19.5;
-    const double full = std::floor(n / (2 * units)), rest = n - full * 2 * units;
-    return full * (pair * k + 1) + (rest > units ? pair * k + 1 : rest > 0 ? alone * k + 1 : 0);
-  }
-  const double few = tile == 256 ? (parts == 1 ? 18.5 : 51) : (parts == 1 ? 12.5 : 31);
-  const double all = tile == 256 ? (parts == 1 ? 26 : 70) : (parts == 1 ? 19.5 : 46);
-  const double full = std::floor(n / units), rest = n / units - full;
-  return full * (all * k + 2) + (rest > 0 ? (few + (all - few) * rest) * k + 2 : 0);
+// Time in us of `n` workgroups of a tile with ks values of k each, in rounds of one workgroup a compute unit (128-wide tiles two): per
+// 1024 k `few` where few units have one, `all` where all have, `pair` where all have two; around them `start` and, with the units that
+// have one, up to `fill`.
+struct NsRound {
+  double few, all, pair, start, fill;
+};
+double ns_rounds(const NsRound& r, int tile, double n, double ks, double units) {
+  const double k = ks / 1024, places = tile == 128 ? 2 * units : units;
+  const double whole = (tile == 128 ? r.pair : r.all) * k + r.start + r.fill, full = std::floor(n / places), rest = (n - full * places) / units;
+  return full * whole + (rest > 1 ? whole : rest > 0 ? (r.few + (r.all - r.few) * rest) * k + r.start + r.fill * rest : 0);
 }
+
+// A and the polynomial in one and in two parts, and X.  Fitted to some 1000 and 500 kernel times, small sides 256 .. 5120, off by 8 to 18% and by 2
+// to 4%.  The cut that ns_cut takes is 1.4% slower than the best of those measured on average, 12% at most (768 x 768); ns_apply_tile takes
+// the faster tile each time.  E.g. A for r = K = 4096, two parts: 228 us in 128-wide tiles (528 of them, two rounds), 186 in 192-wide
+// (253, one round), 232 in 256-wide (136 on 256 units); r = 1024, K = 4096: 81 in one slab, 25 and 5 for joining in four.  X for 1024 x 4096, two
+// parts: 33 in 128-wide tiles, 66 in 256-wide.
+const NsRound kNsHalf[2][3] = {{{9, 10, 12, 8.5, 5}, {10.5, 16, 0, 11.5, 6}, {16, 26, 0, 16.5, 6}},
+                               {{18, 22, 34.5, 11, 4.5}, {28, 43, 0, 16, 6}, {47, 66, 0, 23, 6}}};
+const double kNsSlabStart[2] = {4, 4.5};       // sums go to a slab, not finished to both halves
+const NsRound kNsApply[2][2] = {{{10.3, 10.9, 14.3, 5.4, 2.1}, {17.7, 23.8, 0, 9.9, 6.7}}, {{20.1, 24.2, 37.9, 6.4, 1.4}, {47.9, 68.7, 0, 13, 5.9}}};
 
 constexpr int64_t kNsPad = 64;
 int64_t padded(int64_t n) { return ceil_div(n, kNsPad) * kNsPad; }
@@ -172,7 +177,7 @@ bool linear_takes_few(int64_t T, int64_t out, int64_t in, int dtype) {
 }
 
 // ------------------------------------------------------------------------------------------- orthogonalised updates
-// Slabs only in 128-wide tiles: where they pay there are few tiles.  Joining them costs a launch and their traffic at 4.5 TB/s.
+// Slabs only in 128-wide tiles: where they pay there are few tiles.  Joining them costs a launch and their traffic at 5.3 TB/s.
 NsCut ns_cut(int64_t r, int64_t K, int parts, int compute_units) {
   NsCut best{128, 1, K};
   double least = -1;
@@ -181,8 +186,10 @@ NsCut ns_cut(int64_t r, int64_t K, int parts, int compute_units) {
     for (int slabs = 1; slabs <= (tile == 128 ? 16 : 1); ++slabs) {
       const int64_t ks = padded(ceil_div(K, slabs));
       if (ceil_div(K, ks) != slabs || (slabs > 1 && ks < 128)) continue;
-      double cost = ns_rounds(tile, parts, tiles * slabs, (double)ks, compute_units);
-      if (slabs > 1) cost += 3 + tiles * (slabs + 1) * 65536 / 4.5e6;
+      NsRound round = kNsHalf[parts - 1][tile / 64 - 2];
+      if (slabs > 1) round.start = kNsSlabStart[parts - 1];
+      double cost = ns_rounds(round, tile, tiles * slabs, (double)ks, compute_units);
+      if (slabs > 1) cost += 2 + 0.1 * slabs + tiles * (slabs + 1) * 65536 / 5.3e6;
       if (least < 0 || cost < least) {
         least = cost;
         best = NsCut{tile, slabs, slabs > 1 ? ks : K};
@@ -194,7 +201,7 @@ NsCut ns_cut(int64_t r, int64_t K, int parts, int compute_units) {
 
 int ns_apply_tile(int64_t rows, int64_t cols, int64_t K, int parts, int compute_units) {
   auto cost = [&](int tile) {
-    return ns_rounds(tile, parts, (double)(ceil_div(rows, tile) * ceil_div(cols, tile)), (double)K, compute_units);
+    return ns_rounds(kNsApply[parts - 1][tile / 128 - 1], tile, (double)(ceil_div(rows, tile) * ceil_div(cols, tile)), (double)K, compute_units);
   };
   return cost(256) < cost(128) ? 256 : 128;
 }
