@@ -113,7 +113,8 @@ Cut best_cut(int64_t M, int64_t N, int64_t K, int dtype, int compute_units, Line
     for (int want = 1; want <= 16; ++want) {
       const int64_t ks = ceil_div(ceil_div(K, want), unit) * unit;
       const int64_t slabs = ceil_div(K, ks);
-      if (slabs != want || (want > 1 && ks < 256)) continue;
+      if (want > 1 && ks < 256) break;
+      if (slabs != want) continue;
       if (direct && want > 1 && K - (slabs - 1) * ks < unit) continue;       // a slab of no whole stage has nothing for the direct loads
       double cost = round_cost(dtype, tile, tiles * (double)slabs, (double)ks, compute_units);
       if (dtype != 0 && !direct) cost *= 1.75;
@@ -154,7 +155,8 @@ LinearPlan linear_choice(int64_t M, int64_t N, int64_t K, int dtype, int compute
 
 LinearSpace linear_space(int64_t M, int64_t N, int64_t K, int dtype, int compute_units, bool across) {
   LinearSpace l{0, 0, 0};
-  const LinearPlan pieces = linear_plan(M, N, K, dtype, compute_units, ROWS_IN_PIECES), other = linear_choice(M, N, K, dtype, compute_units, across, false);
+  const LinearPlan pieces = linear_plan(M, N, K, dtype, compute_units, ROWS_IN_PIECES);
+  const LinearPlan other = dtype == 0 ? pieces : linear_choice(M, N, K, dtype, compute_units, across, false);
   const int32_t slabs = pieces.slabs > other.slabs ? pieces.slabs : other.slabs;
   if (slabs > 1) l.slabs = (size_t)slabs * (size_t)M * (size_t)norm_pitch(N) * 4u;
   if (other.pack) {
@@ -185,7 +187,8 @@ NsCut ns_cut(int64_t r, int64_t K, int parts, int compute_units) {
     const double tiles = (double)ns_half_tiles(r, tile);
     for (int slabs = 1; slabs <= (tile == 128 ? 16 : 1); ++slabs) {
       const int64_t ks = padded(ceil_div(K, slabs));
-      if (ceil_div(K, ks) != slabs || (slabs > 1 && ks < 128)) continue;
+      if (slabs > 1 && ks < 128) break;
+      if (ceil_div(K, ks) != slabs) continue;
       NsRound round = kNsHalf[parts - 1][tile / 64 - 2];
       if (slabs > 1) round.start = kNsSlabStart[parts - 1];
       double cost = ns_rounds(round, tile, tiles * slabs, (double)ks, compute_units);
