@@ -37,6 +37,7 @@ extern "C" {
  *   xh = (x - mean) rstd                                     y = w xh + b
  *   h = w dy,  dx = rstd (h - mean_j h - xh mean_j(h xh))    (RMSNORM: without the mean_j h)
  *   dw[j] = sum_t dy[t, j] xh[t, j]                          db[j] = sum_t dy[t, j]
+ * A row whose sum or sum of squares is beyond fp32's range (3.4e38) has rstd 0, and a y that is the shift or no number.
  * ---------------------------------------------------------------------- */
 typedef struct {
   int32_t kind;      /* CHUNKFT_RMSNORM or CHUNKFT_LAYERNORM */

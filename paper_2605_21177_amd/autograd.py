@@ -346,8 +346,8 @@ def chunk_linear(x: torch.Tensor, W: torch.Tensor, seg: Optional[ChunkSegment], 
 
 def chunk_norm(x: torch.Tensor, w: Optional[torch.Tensor], b: Optional[torch.Tensor] = None, kind: int = B.RMSNORM,
                eps: float = 1e-5, seg: Optional[ChunkSegment] = None, bias_seg: Optional[ChunkSegment] = None) -> torch.Tensor:
-    """RMSNORM or LAYERNORM over the last dimension of `x`, times `w` plus `b` (either may be None).  The vectors do not require
-    grad; `seg` and `bias_seg` name their active parts."""
+    """RMSNORM or LAYERNORM over the last dimension of `x`, times `w` plus `b` (either may be None).  The vectors have `x`'s type
+    and do not require grad; `seg` and `bias_seg` name their active parts."""
     n = x.shape[-1]
     for vec, vec_seg, name in ((w, seg, "w"), (b, bias_seg, "b")):
         if vec is not None:

@@ -70,8 +70,9 @@ RowShape norm_forward_shape(int64_t n, int dtype) {
   return {0, 0};
 }
 
-// The backward pass holds more of a row per element: eight elements a lane, sixteen of the widest rows.  With sixteen a lane the
-// registers of a bf16 row spilled: 8192 x 4096 61 us, with eight 41.
+// The backward pass holds more of a row per element: eight elements a lane.  With sixteen a lane the registers of a bf16 row spilled:
+// 8192 x 4096 61 us, with eight 41.  Rows of more than 8192 elements have sixteen all the same, in the one workgroup that holds them, and
+// spill 2 registers (bf16), 12 (fp32) or 32 (fp32, rows that are no whole pieces).
 RowShape norm_backward_shape(int64_t n, int dtype) {
   const int pieces = dtype == 0 ? 2 : 1;
   for (int lanes = 64; lanes <= 1024; lanes *= 2)
