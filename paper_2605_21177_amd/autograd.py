@@ -33,7 +33,9 @@ class ChunkSegment:
 
     Plain mode (`g` given): backward writes the segment's fp32 gradient to `g`
     (`end - begin` elements) on the first micro-batch after `reset()` and adds to
-    it on the following ones. A layer's backward that runs out of memory changes and counts nothing.
+    it on the following ones. A layer's backward that runs out of memory changes and counts
+    nothing, one of whose calls is refused counts nothing that comes behind it; what earlier layers or micro-batches have
+    added stays: `reset()` and repeat them all.
     Fused mode (`master`, `m`, `v`, `hp` given): backward updates the chunk state
     and the segment of `W` in place (a bf16 `W` receives the rounded master, an fp32
     `W` a copy of it; `master` may also be the segment of an fp32 `W` itself, the
@@ -149,15 +151,18 @@ class _VectorGrads:
         return None if self.bufs[i] is None else (seg.begin, seg.end)
 
     def finish(self):
-        for (seg, vec), buf in zip(self.pairs, self.bufs):
-            if buf is None:
-                continue
+        """Updates, which can be refused, and then what only has to be counted: until then a first micro-batch can be repeated."""
+        active = [(seg, vec, buf) for (seg, vec), buf in zip(self.pairs, self.bufs) if buf is not None]
+        for seg, vec, buf in active:
             if seg.fused:
                 B.chunkft_adamw_chunk(buf, seg.master, seg.m, seg.v, vec[seg.begin:seg.end], seg.end - seg.begin, seg.hp,
                                       w_dtype=B._torch_dtype_code(vec))
-            elif not self.direct:
-                seg.g.add_(buf) if seg.micro_batches else seg.g.copy_(buf)
-            seg.one_more()
+                seg.one_more()
+        for seg, _, buf in active:
+            if not seg.fused:
+                if not self.direct:
+                    seg.g.add_(buf) if seg.micro_batches else seg.g.copy_(buf)
+                seg.one_more()
 
 
 class _ChunkLinear(torch.autograd.Function):
@@ -213,9 +218,9 @@ class _LinearLayer(torch.autograd.Function):
             B.chunkft_linear_backward(layer, dy2, Z=z, dZ=dz if z is not None else None, dX=dx, db=grads.bufs[0], b_range=grads.span(0),
                                       accumulate=grads.accumulate, ws=ws)
         if T:
-            grads.finish()
             if weight is not None:
                 weight()
+            grads.finish()
         return (None if dx is None else dx.view(ctx.shape), None, None, dy if ctx.needs_input_grad[3] else None, None, None, None,
                 None, None)
 

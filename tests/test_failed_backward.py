@@ -184,3 +184,31 @@ def test_an_update_that_is_refused_is_not_counted(library):
     step = lambda: A.chunk_norm(x, w, seg=seg).sum().backward()  # noqa: E731
     _twice(library, step, "adamw_chunk", [seg])
     assert seg.micro_batches == 1 and torch.allclose(seg.m, x.sum(0))
+
+
+@pytest.mark.parametrize("kind,failing", [("plain", "chunk_wgrad"), ("adam", "wgrad_adamw_fused"), ("muon", "muon_chunk")])
+def test_a_refused_weight_gradient_leaves_the_bias_to_be_written_again(library, kind, failing):
+    x, W, b, R = _data(7)
+    seg, bias_seg = _segment(kind, 0, 2 * IN), _segment("plain", 0, OUT)
+    step = lambda: (A.chunk_linear(x, W, seg, bias=b, bias_seg=bias_seg) * R).sum().backward()  # noqa: E731
+    library.fail = failing
+    with pytest.raises(B.ChunkFTError):
+        step()
+    assert seg.micro_batches == bias_seg.micro_batches == 0
+    step()
+    assert torch.allclose(_result(seg), (R.t() @ x).reshape(-1)[:2 * IN]) and torch.allclose(bias_seg.g, R.sum(0))
+
+
+@pytest.mark.parametrize("fused_first", [True, False])
+def test_a_refused_update_of_one_vector_leaves_the_other_to_be_written_again(library, fused_first):
+    x, _, _, _ = _data(8)
+    w, b, R = torch.ones(IN), torch.zeros(IN), torch.randn(T, IN, generator=torch.Generator().manual_seed(9))
+    segs = [_segment("adam", 0, IN), _segment("plain", 0, IN)]
+    seg, bias_seg = segs if fused_first else segs[::-1]
+    step = lambda: (A.chunk_norm(x, w, b, B.LAYERNORM, seg=seg, bias_seg=bias_seg) * R).sum().backward()  # noqa: E731
+    library.fail = "adamw_chunk"
+    with pytest.raises(B.ChunkFTError):
+        step()
+    assert seg.micro_batches == bias_seg.micro_batches == 0
+    step()
+    assert torch.allclose(_result(seg), (R * x).sum(0)) and torch.allclose(_result(bias_seg), R.sum(0))
